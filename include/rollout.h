@@ -48,6 +48,7 @@ extern "C" {
 
 #define ROLLOUT_DTYPE_F32 0
 #define ROLLOUT_DTYPE_BF16 1
+#define ROLLOUT_DTYPE_F16 2 /* IEEE half: tensors of the training-side calls only, no model is stored in it */
 
 /* runtime flags */
 #define ROLLOUT_RT_SIMPLE_KERNELS 1u /* run every operator with the plain one-op-per-kernel path */
@@ -351,6 +352,62 @@ int rollout_policy_loss(int32_t n_seqs, const int32_t *cu_seqlens, const float *
                         const float *logp_ref, const uint8_t *mask, const float *rewards,
                         const rollout_loss_params *params, void *hip_stream, float *loss, float *grad,
                         float *advantages);
+
+/* ---- The vocabulary's two ends of a policy-gradient pass --------------------------------------
+ * What stands between a trainer's network and rollout_policy_loss: log-probs of given tokens from the trainer's logits,
+ * or from its hidden states and lm_head matrix, the way back from d loss / d logp, and the embedding rows with their
+ * gradient.  Common to all of these calls:
+ *   - Every array is DEVICE memory on the current device.  The call only enqueues kernels on hip_stream (NULL = the null
+ *     stream): no allocation, no copy, no synchronisation, so it can be captured into a graph; outputs are valid once the
+ *     stream has reached that point.  Nothing is kept between calls, and calls with different workspaces may overlap.
+ *   - workspace: at least the bytes that the matching *_workspace function returns (>= 0, or E_INVAL for sizes that the call
+ *     refuses), aligned to 16 bytes; NULL where that is 0.  Its contents need not be initialised and mean nothing
+ *     afterwards.  Calls and graphs that may run at the same time need one each.
+ *   - dtype: ROLLOUT_DTYPE_F32, _BF16 or _F16.  Strides count elements between rows; inside a row values are consecutive.
+ *     Rows need only be aligned to their elements.
+ *   - Sums are fp32, taken in an order that the sizes fix: the same inputs give the same bits.
+ *   - Errors: E_INVAL, E_HIP; rollout_last_error(NULL) gives the text. */
+
+/* Log-probs of given tokens with entropy and the most likely alternatives.  Of row x with temperature T:
+ *   logp = x_t / T - ln sum_v exp(x_v / T) at t = targets[r]; 0 where targets is NULL or t is outside [0, vocab)
+ *   entropy = - sum_v p_v ln p_v (nats), p = softmax(x / T); values of -inf (ids that may not occur) have no share
+ *   row_stats[r] = (max x, ln sum_v exp((x_v - max x) / T)): what the gradient needs of the row
+ *   top_ids, top_logp [rows][top]: the `top` greatest values, greatest first, equal ones by ascending id, NaN last, and
+ *     their log-probs; 0 <= top <= min(vocab, ROLLOUT_TOP_MAX), both NULL with 0
+ * A row of -inf alone: logp -inf, entropy 0, row_stats (-inf, -inf), alternatives of log-prob -inf.  A row with a NaN or
+ * +inf has NaN for all of its numbers. */
+#define ROLLOUT_TOP_MAX 64
+int64_t rollout_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t top);
+int rollout_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                           float temperature, const int32_t *targets, int32_t top, void *workspace,
+                           size_t workspace_bytes, void *hip_stream, float *logp, float *entropy, float *row_stats,
+                           int32_t *top_ids, float *top_logp);
+
+/* The gradient of sum_r grad_logp[r] logp[r] + grad_entropy[r] entropy[r] with respect to the logits:
+ *   grad_logits_v = [ grad_logp (1{v = t} - p_v) - grad_entropy p_v (ln p_v + entropy) ] / T
+ * row_stats and entropy as rollout_token_logprobs left them for the same logits, temperature and targets; grad_entropy
+ * may be NULL, entropy then too.  grad_logp of a row without a target counts for nothing.  A row whose gradients are
+ * both 0, and a row of -inf alone, gets zeros, its logits unread.  grad_logits has the logits' dtype and may be the
+ * logits array itself with the same row stride; otherwise the two must not overlap.  What lies between the rows is left as it was. */
+int rollout_token_logprobs_grad(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
+                                float temperature, const int32_t *targets, const float *row_stats, const float *entropy,
+                                const float *grad_logp, const float *grad_entropy, void *hip_stream, void *grad_logits,
+                                int64_t grad_row_stride);
+
+/* out[r] = scale * table[tokens[r]], rounded once to dtype; zeros for ids outside [0, vocab) (padding).
+ * table [vocab][hidden], out [n][hidden] without gaps. */
+int rollout_embed(const void *table, int32_t dtype, int32_t vocab, int32_t hidden, int64_t table_stride,
+                  const int32_t *tokens, int32_t n, float scale, void *hip_stream, void *out);
+
+/* The gradient of the embedding matrix: grad_table[v] = base[v] + scale * sum of grad_rows[r] over r with tokens[r] = v,
+ * in the order of r, fp32, rounded once to table_dtype (dtype or ROLLOUT_DTYPE_F32).  Ids outside [0, vocab) add nothing.
+ * base [vocab][hidden] of table_dtype, or NULL (0): a tied matrix takes the gradient of the lm_head here.  base may be
+ * grad_table itself - then rows of ids that do not occur are neither read nor written - and must not overlap it
+ * otherwise.  grad_rows [n][hidden] of dtype; grad_table and base without gaps. */
+int64_t rollout_embed_grad_workspace(int32_t n, int32_t vocab, int32_t hidden);
+int rollout_embed_grad(const void *grad_rows, int32_t dtype, int32_t n, int32_t vocab, int32_t hidden, int64_t row_stride,
+                       const int32_t *tokens, float scale, const void *base, int32_t table_dtype, void *workspace,
+                       size_t workspace_bytes, void *hip_stream, void *grad_table);
 
 /* Parity hook: copies the fp32 logits rows of the last prefill (one per prompt, prompt
  * order) or decode step (one per stepped sample, ascending id) to host `out`

@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "librollout.so")
 
 OK, E_INVAL, E_NOMEM, E_HIP, E_STATE = 0, -1, -2, -3, -4
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 RT_SIMPLE_KERNELS = 1
 RT_RECORD_ROUTING = 2
 RT_KERNEL_TIMING = 4
@@ -126,6 +126,15 @@ SIGNATURES = {
     "rollout_philox_words": (C.c_int, [C.c_uint64, C.c_int32, _P, _P, _P]),
     "rollout_policy_loss": (C.c_int, [C.c_int32, _P, _P, _P, _P, _P, _P, C.POINTER(rollout_loss_params), _P,
                                       C.POINTER(C.c_float), _P, _P]),
+    "rollout_token_logprobs_workspace": (C.c_int64, [C.c_int32] * 3),
+    "rollout_token_logprobs": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_float, _P, C.c_int32, _P,
+                                         C.c_size_t, _P, _P, _P, _P, _P, _P]),
+    "rollout_token_logprobs_grad": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_float, _P, _P, _P,
+                                              _P, _P, _P, _P, C.c_int64]),
+    "rollout_embed": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, C.c_int32, C.c_float, _P, _P]),
+    "rollout_embed_grad_workspace": (C.c_int64, [C.c_int32] * 3),
+    "rollout_embed_grad": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, C.c_float, _P,
+                                     C.c_int32, _P, C.c_size_t, _P, _P]),
     "rollout_pool_create": (_P, [C.c_int32]),
     "rollout_pool_destroy": (None, [_P]),
     "rollout_pool_free_pages": (C.c_int32, [_P]),
@@ -478,6 +487,174 @@ def rollout_policy_loss(cu_seqlens, logp_new, logp_old, logp_ref, mask, rewards,
     if rc != OK:
         raise RolloutError(rc, lib.rollout_last_error(None).decode())
     return loss.value, grad, adv
+
+
+def _refuse(msg):
+    raise RolloutError(E_INVAL, msg)
+
+
+def _dtype_id(t, name):
+    import torch
+    ids = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+    if t.dtype not in ids:
+        _refuse(f"{name} must be float32, bfloat16 or float16")
+    return ids[t.dtype]
+
+
+def _rows(t, name, device, dtype=None, shape=None):
+    """A matrix on `device` whose rows lie anywhere, their values side by side.  Returns its row stride."""
+    if t.dim() != 2 or t.device != device or not t.is_cuda:
+        _refuse(f"{name} must be a matrix on the GPU that holds the other arrays")
+    if dtype is not None and t.dtype != dtype:
+        _refuse(f"{name} must be {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        _refuse(f"{name} must have shape {tuple(shape)}")
+    rows, width = t.shape
+    if width > 1 and t.stride(1) != 1:
+        _refuse(f"{name}: values of a row must be consecutive")
+    if rows <= 1:
+        return width
+    if t.stride(0) < width:
+        _refuse(f"{name}: rows overlap")
+    return t.stride(0)
+
+
+def _vector(t, name, device, dtype, n):
+    if t is None:
+        return None
+    if t.device != device or t.dtype != dtype or t.dim() != 1 or len(t) != n or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} vector of {n} on {device}")
+    return t.data_ptr()
+
+
+class _On:
+    """The device of a call's arrays made current and its stream: `stream`, a handle as elsewhere in this module, or the
+    device's current PyTorch stream.  What is allocated inside belongs to that stream."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.guards = []
+        if torch.cuda.current_device() != device.index:
+            self.guards.append(torch.cuda.device(device))
+        if stream is not None:
+            self.guards.append(torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)))
+        self.handle = stream if stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+    def __enter__(self):
+        for g in self.guards:
+            g.__enter__()
+        return self.handle
+
+    def __exit__(self, *exc):
+        for g in reversed(self.guards):
+            g.__exit__(*exc)
+
+
+def _enqueued(lib, rc):
+    if rc != OK:
+        raise RolloutError(rc, lib.rollout_last_error(None).decode())
+
+
+def _workspace(lib, size, device):
+    """Bytes for one call, from PyTorch's allocator: a graph under capture gets its own."""
+    import torch
+    if size < 0:
+        _enqueued(lib, size)
+    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+
+
+def rollout_token_logprobs(logits, targets=None, *, temperature=1.0, top=0, stream=None):
+    """Log-probs of `targets` (int32 [rows], or None) under logits [rows][vocab] (CUDA, float32 / bfloat16 / float16; rows
+    may be strided), with entropies and the `top` most likely alternatives.  Returns new CUDA tensors (logp, entropy,
+    row_stats [rows][2], top_ids int32 [rows][top], top_logp [rows][top]), the last two None without `top`.  Enqueues on
+    `stream` (a handle; default: PyTorch's current stream) and does not wait: keep the inputs until that work is done."""
+    import torch
+    lib, device = load_library(), logits.device
+    stride = _rows(logits, "logits", device)
+    rows, vocab = logits.shape
+    dtype = _dtype_id(logits, "logits")
+    tgt = _vector(targets, "targets", device, torch.int32, rows)
+    with _On(device, stream) as s:
+        ws = _workspace(lib, lib.rollout_token_logprobs_workspace(rows, vocab, top), device)
+        logp, entropy = torch.empty(rows, device=device), torch.empty(rows, device=device)
+        stats = torch.empty(rows, 2, device=device)
+        ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top else None
+        alt = torch.empty(rows, top, device=device) if top else None
+        _enqueued(lib, lib.rollout_token_logprobs(
+            logits.data_ptr(), dtype, rows, vocab, stride, temperature, tgt, top, ws.data_ptr() if ws is not None else None,
+            len(ws) if ws is not None else 0, s, logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(),
+            ids.data_ptr() if top else None, alt.data_ptr() if top else None))
+    return logp, entropy, stats, ids, alt
+
+
+def rollout_token_logprobs_grad(logits, targets, row_stats, entropy, grad_logp, grad_entropy=None, *, temperature=1.0,
+                                out=None, stream=None):
+    """The gradient of the logits from those of rollout_token_logprobs' logp and (or None) entropy; row_stats and entropy
+    are what it returned.  `out`: where to put it (default: a new tensor); may be `logits` itself."""
+    import torch
+    lib, device = load_library(), logits.device
+    stride = _rows(logits, "logits", device)
+    rows, vocab = logits.shape
+    dtype = _dtype_id(logits, "logits")
+    tgt = _vector(targets, "targets", device, torch.int32, rows)
+    if _rows(row_stats, "row_stats", device, torch.float32, (rows, 2)) != 2:
+        _refuse("row_stats must be contiguous")
+    ent = _vector(entropy, "entropy", device, torch.float32, rows)
+    gl = _vector(grad_logp, "grad_logp", device, torch.float32, rows)
+    ge = _vector(grad_entropy, "grad_entropy", device, torch.float32, rows)
+    out_stride = _rows(out, "out", device, logits.dtype, logits.shape) if out is not None else vocab
+    if out is not None and out.data_ptr() == logits.data_ptr():
+        out_stride = stride  # one row: any stride is its own
+    with _On(device, stream) as s:
+        if out is None:
+            out = torch.empty(rows, vocab, dtype=logits.dtype, device=device)
+        _enqueued(lib, lib.rollout_token_logprobs_grad(logits.data_ptr(), dtype, rows, vocab, stride, temperature, tgt,
+                                                       row_stats.data_ptr(), ent, gl, ge, s, out.data_ptr(), out_stride))
+    return out
+
+
+def rollout_embed(table, tokens, *, scale=1.0, out=None, stream=None):
+    """scale * table[tokens] as [n][hidden] in the table's type; zeros for ids outside the table.  Stream as in
+    rollout_token_logprobs."""
+    import torch
+    lib, device = load_library(), table.device
+    stride = _rows(table, "table", device)
+    vocab, hidden = table.shape
+    dtype = _dtype_id(table, "table")
+    n = len(tokens)
+    tok = _vector(tokens, "tokens", device, torch.int32, n)
+    if out is not None and (_rows(out, "out", device, table.dtype, (n, hidden)) != hidden):
+        _refuse("out must be contiguous")
+    with _On(device, stream) as s:
+        if out is None:
+            out = torch.empty(n, hidden, dtype=table.dtype, device=device)
+        _enqueued(lib, lib.rollout_embed(table.data_ptr(), dtype, vocab, hidden, stride, tok, n, scale, s, out.data_ptr()))
+    return out
+
+
+def rollout_embed_grad(grad_rows, tokens, vocab, *, scale=1.0, base=None, dtype=None, out=None, stream=None):
+    """The gradient of the embedding matrix [vocab][hidden] from that of its rows; `base` is added (a tied lm_head's
+    gradient).  dtype: of the result, default the base's or grad_rows'.  out: where to put it (default: a new tensor);
+    may be `base` itself, which then changes only where an id occurs.  Stream as in rollout_token_logprobs."""
+    import torch
+    lib, device = load_library(), grad_rows.device
+    stride = _rows(grad_rows, "grad_rows", device)
+    n, hidden = grad_rows.shape
+    rows_dtype = _dtype_id(grad_rows, "grad_rows")
+    tok = _vector(tokens, "tokens", device, torch.int32, n)
+    given = next((t for t in (out, base) if t is not None), None)
+    dtype = dtype or (given.dtype if given is not None else grad_rows.dtype)
+    for t, name in ((base, "base"), (out, "out")):
+        if t is not None and _rows(t, name, device, dtype, (vocab, hidden)) != hidden:
+            _refuse(f"{name} must be contiguous")
+    with _On(device, stream) as s:
+        if out is None:
+            out = torch.empty(vocab, hidden, dtype=dtype, device=device)
+        ws = _workspace(lib, lib.rollout_embed_grad_workspace(n, vocab, hidden), device)
+        _enqueued(lib, lib.rollout_embed_grad(grad_rows.data_ptr(), rows_dtype, n, vocab, hidden, stride, tok, scale,
+                                              base.data_ptr() if base is not None else None, _dtype_id(out, "out"),
+                                              ws.data_ptr(), len(ws), s, out.data_ptr()))
+    return out
 
 
 def rollout_philox_words(seed, sample_ids, steps):

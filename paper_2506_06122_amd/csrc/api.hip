@@ -9,34 +9,9 @@
 #include <mutex>
 #include <thread>
 
+#include "api_guard.h"
 #include "engine.h"
 #include "tile_plan.h"
-
-static thread_local std::string g_init_error;
-
-static void fail(int code, const std::string& msg) { throw ApiError{code, msg}; }
-
-template <typename F>
-static int guarded(rollout_ctx* ctx, F&& body) {
-  std::string* err = ctx ? &ctx->err : &g_init_error;
-  try {
-    body();
-    return ROLLOUT_OK;
-  } catch (const ApiError& e) {
-    *err = e.msg;
-    return e.code;
-  } catch (const HipError& e) {
-    *err = std::string("HIP error ") + hipGetErrorString(e.code) + " in " + e.expr + " (" + e.file + ":" +
-           std::to_string(e.line) + ")";
-    return ROLLOUT_E_HIP;
-  } catch (const std::bad_alloc&) {
-    *err = "host allocation failed";
-    return ROLLOUT_E_NOMEM;
-  } catch (...) {
-    *err = "unexpected internal error";
-    return ROLLOUT_E_STATE;
-  }
-}
 
 static void h2d(void* dst, const void* src, size_t bytes, hipStream_t s) {
   if (bytes) HIP_TRY(hipMemcpyAsync(dst, src, bytes, hipMemcpyHostToDevice, s));

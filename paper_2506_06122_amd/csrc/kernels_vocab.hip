@@ -1,0 +1,407 @@
+// Log-probs of given tokens from logits, with entropy and the most likely alternatives, and the gradient of the logits.
+//
+//   y_v = (x_v - m) log2(e) / T,  S = sum 2^y,  ln p_v = ln2 y_v - ln S,  H = ln S - ln2 (sum y 2^y) / S
+//
+// One pass over the row: every thread keeps the maximum it has seen, and its two sums relative to that; a chunk of values
+// is taken relative to the new maximum, the old sums are scaled once a chunk.  The pass is bound by memory; the arithmetic
+// (11 issue slots per value, the exponential counting four) comes next.
+//
+// Alternatives ride along for free: the K-th largest of the threads' maxima is a bound that K values reach, and every value
+// that reaches it sits with a thread whose maximum does.  So only those threads' values are read again, spread over the
+// workgroup, and what reaches the bound - a few more than K - is ranked.  Rows that defeat this (long runs of equal values,
+// NaN) are found one alternative per sweep instead.
+//
+// A row belongs to one workgroup where rows are enough; fewer are cut into parts whose results a second launch joins.
+#include "vocab.h"
+#include "vocab_vec.h"
+
+#include <algorithm>
+
+namespace {
+
+constexpr int T = kTokenThreads, NW = T / WAVE;
+constexpr int kListed = 1024;       // candidates a workgroup can rank
+constexpr int kPartValues = 2048;   // fewest values worth a workgroup
+constexpr int kFill = 1024;         // workgroups that fill the card
+
+// Order of the alternatives: greater values first, then lower ids; -0 and 0 are equal, NaN comes last.  Key 0 is nothing.
+__device__ inline unsigned value_key(float x) {
+  if (x != x) return 1;
+  const unsigned u = __float_as_uint(x + 0.f);  // -0 + 0 = 0
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ inline float key_value(unsigned k) {
+  if (k <= 1) return __uint_as_float(0x7fc00000u);
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
+__device__ inline unsigned long long full_key(unsigned key, int id) { return (unsigned long long)key << 32 | (unsigned)~id; }
+
+// How a row lies in memory: `head` values up to the first 16-byte boundary, `vecs` vectors, `tail` values.  A part takes
+// vectors [begin, end), the first part the head, the last the tail.
+template <typename V>
+struct RowSlice {
+  const V* x;
+  int head, begin, end, tail_at, tail;
+  __device__ RowSlice(const V* row, int vocab, int part, int parts) {
+    constexpr int E = kVec<V>;
+    x = row;
+    head = min(vocab, (int)((16 - ((size_t)row & 15)) & 15) / (int)sizeof(V));
+    const int vecs = (vocab - head) / E, per = (vecs + parts - 1) / parts;
+    begin = min(vecs, part * per);
+    end = min(vecs, begin + per);
+    tail_at = head + vecs * E;
+    tail = part == parts - 1 ? vocab - tail_at : 0;
+    if (part) head_here = 0;
+    else head_here = head;
+  }
+  int head_here;
+  __device__ u32x4 vec(int i) const { return *(const u32x4*)(x + head + (long long)i * kVec<V>); }
+  __device__ int id(int i) const { return head + i * kVec<V>; }
+  // the single value of thread `tid`: one of the head, or one of the tail; -1: none
+  __device__ int single(int tid) const {
+    if (tid < head_here) return tid;
+    return tid >= WAVE && tid - WAVE < tail ? tail_at + tid - WAVE : -1;
+  }
+  __device__ int values() const { return head_here + (end - begin) * kVec<V> + tail; }
+};
+
+template <int N>
+__device__ inline void add_chunk(RowSums& r, const float* v, float c) {
+  float top = v[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+  const float m = fmaxf(r.m, top), d = fminf((m - r.m) * c, 1e30f), f = __builtin_amdgcn_exp2f(-d);
+  r.t = (r.t - d * r.s) * f;
+  r.s *= f;
+  r.m = m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float y = (v[i] - m) * c, e = __builtin_amdgcn_exp2f(y);
+    r.s += e;
+    r.t = fmaf(e, fmaxf(y, -1e30f), r.t);
+  }
+}
+
+__device__ inline RowSums merge_wave(RowSums r, float c) {
+#pragma unroll
+  for (int o = 1; o < WAVE; o <<= 1)
+    r = merge(r, RowSums{__shfl_xor(r.m, o, WAVE), __shfl_xor(r.s, o, WAVE), __shfl_xor(r.t, o, WAVE)}, c);
+  return r;
+}
+
+struct TopShared {
+  unsigned max_key[T];
+  unsigned short hot[T];
+  unsigned bound;
+  int n_hot, n_listed;
+  unsigned long long best[NW];
+  unsigned long long listed[kListed];
+};
+
+// The K greatest keys of the slice, greatest first, through emit(rank, key); ranks past the slice's values get key 0.
+// top: the thread's own maximum (no value: has = false).
+template <typename V, typename Emit>
+__device__ void top_of_slice(const RowSlice<V>& row, float top, bool has, int K, TopShared& sh, Emit&& emit) {
+  constexpr int E = kVec<V>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  sh.max_key[tid] = has ? value_key(top) : 0;
+  if (tid == 0) sh.n_hot = sh.n_listed = 0;
+  __syncthreads();
+  if (wave == 0) {
+    unsigned k[T / WAVE];
+#pragma unroll
+    for (int i = 0; i < T / WAVE; ++i) k[i] = sh.max_key[lane + i * WAVE];
+    unsigned bound = 0;
+    for (int bit = 31; bit >= 0; --bit) {
+      const unsigned trial = bound | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < T / WAVE; ++i) n += __popcll(__ballot(k[i] >= trial));
+      if (n >= K) bound = trial;
+      if (n == K) break;
+    }
+    if (lane == 0) sh.bound = max(bound, 1u);
+  }
+  __syncthreads();
+  const unsigned bound = sh.bound;
+  if (sh.max_key[tid] >= bound) sh.hot[atomicAdd(&sh.n_hot, 1)] = (unsigned short)tid;
+  auto consider = [&](float x, int id) {
+    const unsigned key = value_key(x);
+    if (key >= bound) {
+      const int at = atomicAdd(&sh.n_listed, 1);
+      if (at < kListed) sh.listed[at] = full_key(key, id);
+    }
+  };
+  const int one = row.single(tid);
+  if (one >= 0) consider(to_f32(row.x[one]), one);
+  __syncthreads();
+  const int steps = (row.end - row.begin + T - 1) / T;
+  for (int w = tid; w < sh.n_hot * steps; w += T) {
+    const int i = row.begin + sh.hot[w / steps] + w % steps * T;
+    if (i >= row.end) continue;
+    float v[E];
+    widen(row.vec(i), v, V{});
+#pragma unroll
+    for (int e = 0; e < E; ++e) consider(v[e], row.id(i) + e);
+  }
+  __syncthreads();
+  const int n = sh.n_listed, want = min(K, row.values());
+  if (n <= kListed && n >= want) {
+    for (int i = tid; i < n; i += T) {
+      const unsigned long long mine = sh.listed[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += sh.listed[j] > mine;
+      if (rank < want) emit(rank, mine);
+    }
+  } else {
+    unsigned long long last = ~0ull;
+    for (int k = 0; k < want; ++k) {  // the greatest key below the last one
+      unsigned long long best = 0;
+      auto take = [&](float x, int id) {
+        const unsigned long long key = full_key(value_key(x), id);
+        if (key < last && key > best) best = key;
+      };
+      if (one >= 0) take(to_f32(row.x[one]), one);
+      for (int i = row.begin + tid; i < row.end; i += T) {
+        float v[E];
+        widen(row.vec(i), v, V{});
+#pragma unroll
+        for (int e = 0; e < E; ++e) take(v[e], row.id(i) + e);
+      }
+#pragma unroll
+      for (int o = 1; o < WAVE; o <<= 1) best = max(best, (unsigned long long)__shfl_xor(best, o, WAVE));
+      if (lane == 0) sh.best[wave] = best;
+      __syncthreads();
+      last = max(max(sh.best[0], sh.best[1]), max(sh.best[2], sh.best[3]));
+      if (tid == 0) emit(k, last);
+      __syncthreads();
+    }
+  }
+  for (int k = want + tid; k < K; k += T) emit(k, 0ull);
+}
+
+struct TokenParts {
+  int parts;
+  RowSums* sums;             // [rows][parts]
+  unsigned long long* keys;  // [rows][parts][top]
+};
+
+__device__ inline void store_top(const TokenOut& o, int row, int rank, unsigned long long key, float m, float log_s, float inv_temp) {
+  const long long at = (long long)row * o.top + rank;
+  o.top_ids[at] = (int)~(unsigned)key;
+  o.top_logp[at] = log_s == -INFINITY ? -INFINITY : (key_value((unsigned)(key >> 32)) - m) * inv_temp - log_s;
+}
+
+template <typename V, bool TOP>
+__global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOut out, TokenParts p) {
+  constexpr int E = kVec<V>, U = 4;
+  __shared__ RowSums wave_s[NW];
+  __shared__ float log_s_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
+  const RowSlice<V> row((const V*)in.logits + r * in.stride, in.vocab, part, p.parts);
+  const float c = in.inv_temp * kLog2e;
+  const int target = in.targets ? in.targets[r] : -1;
+  const bool has_target = target >= 0 && target < in.vocab;
+  const float x_target = has_target && p.parts == 1 ? to_f32(row.x[target]) : 0.f;
+  // the reference starts at the lowest finite value: a row of -inf then has differences of -inf, not NaN
+  RowSums sums{-3.402823466e38f, 0.f, 0.f};
+  float single = -INFINITY;
+  const int one = row.single(tid);
+  if (one >= 0) single = to_f32(row.x[one]);
+  int i = row.begin + tid;
+  for (; i + (U - 1) * T < row.end; i += U * T) {
+    u32x4 w[U];
+    float v[U * E];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = row.vec(i + u * T);
+#pragma unroll
+    for (int u = 0; u < U; ++u) widen(w[u], v + u * E, V{});
+    add_chunk<U * E>(sums, v, c);
+  }
+  const bool has = one >= 0 || row.begin + tid < row.end;
+  {
+    u32x4 w[U];
+    float v[U * E];
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (i + u * T < row.end) w[u] = row.vec(i + u * T);
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (i + u * T < row.end) {
+        widen(w[u], v, V{});
+        add_chunk<E>(sums, v, c);
+      }
+    if (one >= 0) add_chunk<1>(sums, &single, c);
+  }
+  // (what starts at the lowest finite value stays there when every value is -inf; both order alike below any other)
+  const RowSums all = merge_wave(sums, c);
+  if (lane == 0) wave_s[wave] = all;
+  __syncthreads();
+  RowSums total = wave_s[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) total = merge(total, wave_s[w], c);
+  if (p.parts == 1) {
+    if (tid == 0) log_s_s = finish_row(total, out, r, has_target, x_target, in.inv_temp);
+  } else if (tid == 0) {
+    p.sums[(long long)r * p.parts + part] = total;
+  }
+  if constexpr (TOP) {
+    __shared__ TopShared sh;
+    __syncthreads();
+    const float log_s = p.parts == 1 ? log_s_s : 0.f;
+    // a maximum that is still the start stands for -inf: the bound must not lie above the values themselves
+    const float top = sums.m == -3.402823466e38f ? -INFINITY : sums.m;
+    top_of_slice(row, top, has, out.top, sh, [&](int rank, unsigned long long key) {
+      if (p.parts == 1) store_top(out, r, rank, key, total.m, log_s, in.inv_temp);
+      else p.keys[((long long)r * p.parts + part) * out.top + rank] = key;
+    });
+  }
+}
+
+// Joins a row's parts.  An alternative of the row is one of its part; keys below the greatest of the parts' last keys
+// cannot be among the first K.
+template <typename V, bool TOP>
+__global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut out, TokenParts p) {
+  __shared__ RowSums wave_s[NW];
+  __shared__ float log_s_s;
+  __shared__ unsigned long long least_s;
+  __shared__ int n_s;
+  extern __shared__ unsigned long long listed[];  // [parts * top]
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x;
+  const float c = in.inv_temp * kLog2e;
+  const int target = in.targets ? in.targets[r] : -1;
+  const bool has_target = target >= 0 && target < in.vocab;
+  const float x_target = has_target ? to_f32(((const V*)in.logits + r * in.stride)[target]) : 0.f;
+  if (tid == 0) {
+    n_s = 0;
+    least_s = 0;
+  }
+  RowSums mine{-3.402823466e38f, 0.f, 0.f};
+  for (int i = tid; i < p.parts; i += T) mine = merge(mine, p.sums[(long long)r * p.parts + i], c);
+  mine = merge_wave(mine, c);
+  if (lane == 0) wave_s[wave] = mine;
+  __syncthreads();
+  RowSums total = wave_s[0];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) total = merge(total, wave_s[w], c);
+  if (tid == 0) log_s_s = finish_row(total, out, r, has_target, x_target, in.inv_temp);
+  if constexpr (TOP) {
+    const unsigned long long* keys = p.keys + (long long)r * p.parts * out.top;
+    for (int i = tid; i < p.parts; i += T) atomicMax(&least_s, keys[(long long)i * out.top + out.top - 1]);
+    __syncthreads();
+    const unsigned long long least = max(least_s, 1ull);
+    for (int i = tid; i < p.parts * out.top; i += T) {
+      const unsigned long long key = keys[i];
+      if (key >= least) listed[atomicAdd(&n_s, 1)] = key;
+    }
+    __syncthreads();
+    const int n = n_s;
+    for (int i = tid; i < n; i += T) {
+      const unsigned long long key = listed[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += listed[j] > key;
+      if (rank < out.top) store_top(out, r, rank, key, total.m, log_s_s, in.inv_temp);
+    }
+  }
+}
+
+// dx_v = [g (1{v = t} - p_v) - h p_v (ln p_v + H)] / T, value by value; a row without a gradient is written without being
+// read.  SAME: rows of both arrays lie alike relative to 16 bytes.
+template <typename V, bool SAME>
+__global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
+  constexpr int E = kVec<V>, U = 4;
+  const int tid = threadIdx.x, r = blockIdx.x / parts, part = blockIdx.x % parts;
+  const RowSlice<V> row((const V*)a.in.logits + r * a.in.stride, a.in.vocab, part, parts);
+  V* out = (V*)a.out + r * a.out_stride;
+  const RowGrad g = row_grad(a.row_stats, a.entropy, a.grad_logp, a.grad_entropy, a.in.targets, a.in.inv_temp, a.in.vocab, r);
+  const float c = a.in.inv_temp * kLog2e;
+  auto store = [&](int i, const float* v) {
+    if constexpr (SAME) {
+      *(u32x4*)(out + row.id(i)) = narrow(v, V{});
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) out[row.id(i) + e] = narrow1(v[e], V{});
+    }
+  };
+  const int one = row.single(tid);
+  if (g.none) {
+    float zero[E] = {};
+    for (int i = row.begin + tid; i < row.end; i += T) store(i, zero);
+    if (one >= 0) out[one] = narrow1(0.f, V{});
+    return;
+  }
+  auto apply = [&](u32x4 w, int i) {
+    float v[E];
+    widen(w, v, V{});
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = grad_of(v[e], c, g);
+    const unsigned at = (unsigned)(g.target - row.id(i));
+    if (at < E) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += at == e ? g.at_target : 0.f;
+    }
+    store(i, v);
+  };
+  int i = row.begin + tid;
+  for (; i + (U - 1) * T < row.end; i += U * T) {
+    u32x4 w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = row.vec(i + u * T);
+#pragma unroll
+    for (int u = 0; u < U; ++u) apply(w[u], i + u * T);
+  }
+  for (; i < row.end; i += T) apply(row.vec(i), i);
+  if (one >= 0) out[one] = narrow1(grad_of(to_f32(row.x[one]), c, g) + (one == g.target ? g.at_target : 0.f), V{});
+}
+
+TokenParts layout(int rows, int vocab, int top, void* ws) {
+  TokenParts p{};
+  p.parts = token_parts(rows, vocab);
+  p.keys = (unsigned long long*)ws;
+  p.sums = (RowSums*)(p.keys + (size_t)rows * p.parts * top);
+  return p;
+}
+
+template <typename V>
+void launch(const TokenRows& in, const TokenOut& out, const TokenParts& p, hipStream_t s) {
+  const int grid = in.rows * p.parts;
+  if (out.top) token_logprobs_kernel<V, true><<<grid, T, 0, s>>>(in, out, p);
+  else token_logprobs_kernel<V, false><<<grid, T, 0, s>>>(in, out, p);
+  if (p.parts == 1) return;
+  if (out.top) token_join_kernel<V, true><<<in.rows, T, (size_t)p.parts * out.top * 8, s>>>(in, out, p);
+  else token_join_kernel<V, false><<<in.rows, T, 0, s>>>(in, out, p);
+}
+
+template <typename V>
+void launch_grad(const TokenGrad& a, int parts, hipStream_t s) {
+  const size_t size = sizeof(V);
+  const bool same = (((size_t)a.in.logits - (size_t)a.out) & 15) == 0 && ((a.in.stride - a.out_stride) * size & 15) == 0;
+  const int grid = a.in.rows * parts;
+  if (same) token_grad_kernel<V, true><<<grid, T, 0, s>>>(a, parts);
+  else token_grad_kernel<V, false><<<grid, T, 0, s>>>(a, parts);
+}
+
+}  // namespace
+
+// Parts of a row: as many workgroups as fill the card, none with fewer than kPartValues values, at most 64 (64 x 64 keys
+// are 32 KB of LDS in the join).
+int token_parts(int rows, int vocab) {
+  return std::max(1, std::min({ceil_div(kFill, std::max(rows, 1)), vocab / kPartValues, 64}));
+}
+size_t token_workspace(int rows, int vocab, int top) {
+  const int parts = token_parts(rows, vocab);
+  return parts == 1 ? 0 : (size_t)rows * parts * (sizeof(RowSums) + 8 * (size_t)top);
+}
+void launch_token_logprobs(const TokenRows& in, const TokenOut& out, void* ws, hipStream_t s) {
+  const TokenParts p = layout(in.rows, in.vocab, out.top, ws);
+  if (in.dtype == VT_F32) launch<float>(in, out, p, s);
+  else if (in.dtype == VT_BF16) launch<bf16_t>(in, out, p, s);
+  else launch<f16_t>(in, out, p, s);
+}
+void launch_token_logprobs_grad(const TokenGrad& a, hipStream_t s) {
+  const int parts = token_parts(a.in.rows, a.in.vocab);
+  if (a.in.dtype == VT_F32) launch_grad<float>(a, parts, s);
+  else if (a.in.dtype == VT_BF16) launch_grad<bf16_t>(a, parts, s);
+  else launch_grad<f16_t>(a, parts, s);
+}

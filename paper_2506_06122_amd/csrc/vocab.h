@@ -1,0 +1,121 @@
+// Host-callable launchers of the operators at the vocabulary's two ends of a policy-gradient pass (api_vocab.hip):
+// log-probs of given tokens from logits with their gradient, the same from hidden states and the lm_head matrix, embedding
+// lookup and gradient.  All launches are asynchronous on the given stream; every pointer is device memory the caller owns.
+#pragma once
+#include "common.h"
+
+// Element type of a caller's tensor: ROLLOUT_DTYPE_*.
+enum { VT_F32 = 0, VT_BF16 = 1, VT_F16 = 2 };
+constexpr size_t vt_size(int dtype) { return dtype == VT_F32 ? 4 : 2; }
+
+constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
+
+// ---- logits ------------------------------------------------------------------------------
+constexpr int kTopMax = 64;        // alternatives per row
+constexpr int kTokenThreads = 256;
+
+struct TokenRows {
+  const void* logits;
+  long long stride;  // elements between rows
+  int dtype, rows, vocab;
+  float inv_temp;
+  const int* targets;  // [rows] or NULL; ids outside [0, vocab): no target
+};
+// What one pass leaves of (a part of) a row: reference m (the maximum, at least the lowest finite float), sum 2^y and
+// sum y 2^y with y = (x - m) log2(e) / T.
+struct RowSums {
+  float m, s, t;
+};
+struct TokenOut {
+  float* logp;       // [rows]
+  float* entropy;    // [rows]
+  float* row_stats;  // [rows][2]: maximum, ln of the sum of exp((x - maximum) / T)
+  int top;
+  int* top_ids;      // [rows][top]
+  float* top_logp;   // [rows][top]
+};
+// workgroups a row is cut into
+int token_parts(int rows, int vocab);
+size_t token_workspace(int rows, int vocab, int top);
+void launch_token_logprobs(const TokenRows& in, const TokenOut& out, void* workspace, hipStream_t s);
+
+struct TokenGrad {
+  TokenRows in;
+  const float *row_stats, *entropy;          // as launch_token_logprobs left them; entropy only with grad_entropy
+  const float *grad_logp, *grad_entropy;     // [rows]; grad_entropy may be NULL
+  void* out;                                 // [rows][vocab], in.dtype; may be in.logits
+  long long out_stride;
+};
+void launch_token_logprobs_grad(const TokenGrad& a, hipStream_t s);
+
+// What a row's gradient needs beside its logits: dx = p (a + b y2) (+ at_target at the target), y2 = log2 p.
+struct RowGrad {
+  float m, l2, a, b, at_target;
+  int target;   // -1: none
+  bool none;    // the whole row is zero
+};
+__device__ inline RowGrad row_grad(const float* row_stats, const float* entropy, const float* grad_logp,
+                                   const float* grad_entropy, const int* targets, float inv_temp, int vocab, int row) {
+  RowGrad r;
+  const float l = row_stats[2 * row + 1];
+  const int t = targets ? targets[row] : -1;
+  r.target = t >= 0 && t < vocab ? t : -1;
+  const float gl = grad_logp[row], g = r.target < 0 ? 0.f : gl;
+  const float h = grad_entropy ? grad_entropy[row] : 0.f;
+  r.m = row_stats[2 * row];
+  r.l2 = l * kLog2e;
+  r.none = (g == 0.f && h == 0.f) || l == -INFINITY;
+  r.a = inv_temp * (grad_entropy ? -g - h * entropy[row] : -g);
+  r.b = -h * inv_temp * kLn2;
+  r.at_target = g * inv_temp;
+  return r;
+}
+// c = log2(e) / T.  A banned id has x = -inf: p = 0, and its log2 p must not meet that 0 as an infinity; a NaN stays one.
+__device__ inline float grad_of(float x, float c, const RowGrad& r) {
+  const float y = fmaf(x - r.m, c, -r.l2);
+  return __builtin_amdgcn_exp2f(y) * fmaf(r.b, fmaxf(y, -1e30f), r.a);
+}
+
+__device__ inline RowSums merge(const RowSums& p, const RowSums& q, float c) {
+  const float m = fmaxf(p.m, q.m);
+  // a difference past 1e30 is as good as infinite, and 0 x infinity would be NaN
+  const float dp = fminf((m - p.m) * c, 1e30f), dq = fminf((m - q.m) * c, 1e30f);
+  const float fp = __builtin_amdgcn_exp2f(-dp), fq = __builtin_amdgcn_exp2f(-dq);
+  return RowSums{m, p.s * fp + q.s * fq, (p.t - dp * p.s) * fp + (q.t - dq * q.s) * fq};
+}
+// A row's results from its sums, written by one thread; x_target is read only with a target.  Returns ln S.
+__device__ inline float finish_row(const RowSums& r, const TokenOut& o, int row, bool has_target, float x_target, float inv_temp) {
+  const bool empty = r.s == 0.f;  // nothing but -inf
+  const float log_s = empty ? -INFINITY : logf(r.s);
+  o.logp[row] = !has_target ? 0.f : empty ? -INFINITY : (x_target - r.m) * inv_temp - log_s;
+  o.entropy[row] = empty ? 0.f : log_s - kLn2 * (r.t / r.s);
+  o.row_stats[2 * row] = empty ? -INFINITY : r.m;
+  o.row_stats[2 * row + 1] = log_s;
+  return log_s;
+}
+
+// ---- embedding ---------------------------------------------------------------------------
+struct EmbedArgs {
+  const void* table;
+  long long table_stride;
+  int dtype, vocab, hidden;
+  const int* tokens;
+  int n;
+  float scale;
+  void* out;  // [n][hidden]
+};
+void launch_embed_rows(const EmbedArgs& a, hipStream_t s);
+
+struct EmbedGrad {
+  const void* grad_rows;  // [n][hidden]
+  long long row_stride;
+  int dtype;
+  const int* tokens;
+  int n, vocab, hidden;
+  float scale;
+  const void* base;       // [vocab][hidden], out_dtype, or NULL; may be out
+  int out_dtype;
+  void* out;              // [vocab][hidden]
+};
+size_t embed_grad_workspace(int n, int vocab, int hidden);
+void launch_embed_grad(const EmbedGrad& a, void* workspace, hipStream_t s);

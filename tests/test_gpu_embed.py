@@ -1,0 +1,157 @@
+"""Embedding lookup and the embedding matrix's gradient against oracle/vocab.py.
+
+A looked-up value is one fp32 product rounded to its type.  A gradient is a sum of at most n terms in fp32, added one after
+another: off by n 2^-24 of the sum of magnitudes at most, then scaled, added to the base and rounded to its type."""
+import numpy as np
+import pytest
+
+from oracle import vocab as O
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+TYPES = ["float32", "bfloat16", "float16"]
+
+
+def half_step(dtype, v):
+    eps, least = {"float32": (2.0 ** -24, 2.0 ** -150), "bfloat16": (2.0 ** -8, 2.0 ** -134), "float16": (2.0 ** -11, 2.0 ** -25)}[dtype]
+    return eps * np.abs(v) + least
+
+
+def cuda(a, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(getattr(torch, dtype))
+
+
+def host(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def ids_of(kind, n, vocab, seed):
+    rng = np.random.default_rng(seed)
+    if kind == "same":
+        return np.full(n, vocab - 1, np.int32)
+    if kind == "ordered":
+        return np.sort(rng.integers(0, vocab, n)).astype(np.int32)
+    ids = (rng.random(n) ** 4 * vocab).astype(np.int32)
+    if kind == "padded":
+        ids[rng.random(n) < 0.3] = -1
+        ids[rng.random(n) < 0.1] = vocab
+        ids[rng.random(n) < 0.3] = vocab // 2
+    return ids
+
+
+@pytest.mark.parametrize("n,vocab,hidden", [(1, 1, 1), (5, 9, 7), (187, 4096, 1536), (64, 33, 40), (1000, 151, 20)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_lookup(n, vocab, hidden, dtype):
+    import torch
+    import paper_2506_06122_amd as R
+    rng = np.random.default_rng(n)
+    for pad, shift, scale in ((0, 0, 1.0), (3, 1, 1.0), (8, 0, 59.875), (0, 1, 0.3)):
+        buf = torch.zeros(shift + vocab * (hidden + pad), dtype=getattr(torch, dtype), device="cuda")
+        table = buf[shift:].as_strided((vocab, hidden), (hidden + pad, 1))
+        table.copy_(torch.from_numpy(rng.normal(0, 0.02, (vocab, hidden)).astype(np.float32)))
+        ids = ids_of("padded", n, vocab, 3)
+        got = R.rollout_embed(table, cuda(ids), scale=scale)
+        assert got.dtype == table.dtype and got.shape == (n, hidden)
+        want = O.embed(host(table), ids, float(np.float32(scale)))
+        if scale == 1.0:
+            assert np.array_equal(host(got), want)
+        else:
+            assert np.all(np.abs(host(got) - want) <= half_step(dtype, want) * 1.001 + 2 * U * np.abs(want))
+
+
+@pytest.mark.parametrize("kind", ["padded", "same", "ordered", "spread"])
+@pytest.mark.parametrize("n,vocab,hidden", [(1, 1, 1), (3, 5, 8), (16, 700, 24), (17, 700, 7), (33, 2, 64), (1021, 4096, 96),
+                                            (3000, 40000, 40), (2100, 513, 130)])
+def test_gradient(kind, n, vocab, hidden):
+    import torch
+    import paper_2506_06122_amd as R
+    for i, (dtype, out_type, with_base, pad) in enumerate([("float32", "float32", False, 0), ("bfloat16", "bfloat16", True, 8),
+                                                           ("float16", "float32", True, 1), ("bfloat16", "float32", False, 0),
+                                                           ("float16", "float16", False, 0)]):
+        rng = np.random.default_rng(i)
+        ids = ids_of(kind, n, vocab, i)
+        buf = torch.zeros(n * (hidden + pad), dtype=getattr(torch, dtype), device="cuda")
+        dy = buf.as_strided((n, hidden), (hidden + pad, 1))
+        dy.copy_(torch.from_numpy(rng.normal(0, 1, (n, hidden)).astype(np.float32)))
+        base = cuda(rng.normal(0, 1, (vocab, hidden)).astype(np.float32), out_type) if with_base else None
+        scale = float(np.float32(0.75))
+        got = R.rollout_embed_grad(dy, cuda(ids), vocab, scale=scale, base=base, dtype=getattr(torch, out_type))
+        assert got.dtype == getattr(torch, out_type) and got.shape == (vocab, hidden)
+        b = None if base is None else host(base)
+        want = O.embed_grad(host(dy), ids, vocab, scale, b)
+        mass = O.embed_grad(np.abs(host(dy)), ids, vocab, scale)
+        count = np.bincount(ids[(ids >= 0) & (ids < vocab)], minlength=vocab)[:, None]
+        tol = (count + 2) * U * mass + 2 * U * np.abs(want)
+        assert np.all(np.abs(host(got) - want) <= tol + half_step(out_type, np.abs(want) + tol) * 1.001)
+        again = R.rollout_embed_grad(dy, cuda(ids), vocab, scale=scale, base=base, dtype=getattr(torch, out_type))
+        assert torch.equal(got, again)
+        if base is not None:   # in place: rows of absent ids stay as they are, bit for bit
+            held = base.clone()
+            into = R.rollout_embed_grad(dy, cuda(ids), vocab, scale=scale, base=base, out=base)
+            assert into.data_ptr() == base.data_ptr() and torch.equal(base, got)
+            absent = cuda(count[:, 0] == 0)
+            assert torch.equal(base[absent], held[absent])
+
+
+def test_gradient_of_no_rows_and_of_misaligned_arrays():
+    import torch
+    import paper_2506_06122_amd as R
+    none, ids = torch.zeros(0, 24, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    assert not R.rollout_embed_grad(none, ids, 7).any()
+    base = torch.ones(7, 24, device="cuda")
+    assert torch.equal(R.rollout_embed_grad(none, ids, 7, base=base), base)
+    rng = np.random.default_rng(2)
+    buf = torch.zeros(3 + 50 * 16, dtype=torch.bfloat16, device="cuda")
+    dy = buf[3:].view(50, 16)
+    dy.copy_(torch.from_numpy(rng.normal(size=(50, 16)).astype(np.float32)))
+    out = torch.full((1 + 9 * 16 + 1,), 7.0, dtype=torch.bfloat16, device="cuda")
+    ids = ids_of("padded", 50, 9, 1)
+    got = R.rollout_embed_grad(dy, cuda(ids), 9, out=out[1:-1].view(9, 16))
+    want = O.embed_grad(host(dy), ids, 9, 1.0)
+    assert np.all(np.abs(host(got) - want) <= half_step("bfloat16", want) * 1.01 + 50 * U * 50)
+    assert out[0] == 7.0 and out[-1] == 7.0
+
+
+def test_a_large_batch_of_one_id_and_a_large_vocabulary():
+    import torch
+    import paper_2506_06122_amd as R
+    n, vocab, hidden = 20000, 152064, 64
+    for ids in (np.full(n, 13, np.int32), ids_of("spread", n, vocab, 1)):
+        dy = torch.randn(n, hidden, device="cuda").to(torch.bfloat16)
+        got = host(R.rollout_embed_grad(dy, cuda(ids), vocab, dtype=torch.float32))
+        want = np.zeros((vocab, hidden))
+        np.add.at(want, ids, host(dy))
+        mass = np.zeros((vocab, hidden))
+        np.add.at(mass, ids, np.abs(host(dy)))
+        # sums of 16 rows, then of those sums: 16 + n / 16 additions one after another
+        assert np.all(np.abs(got - want) <= (18 + n / 16) * U * mass)
+
+
+def test_streams_and_graphs():
+    import torch
+    import paper_2506_06122_amd as R
+    ids = cuda(ids_of("padded", 700, 1000, 4))
+    dy, table = torch.randn(700, 48, device="cuda"), torch.randn(1000, 48, device="cuda")
+
+    def both(dy, stream=None):
+        return R.rollout_embed(table, ids, scale=2.0, stream=stream), R.rollout_embed_grad(dy, ids, 1000, base=table, stream=stream)
+
+    want = both(dy)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = both(dy, side.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    held = dy.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(held)
+    for _ in range(3):
+        y = torch.randn_like(dy)
+        want = both(y)
+        held.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, want))
