@@ -364,7 +364,7 @@ int rollout_policy_loss(int32_t n_seqs, const int32_t *cu_seqlens, const float *
  *     refuses), aligned to 16 bytes; NULL where that is 0.  Its contents need not be initialised and mean nothing
  *     afterwards.  Calls and graphs that may run at the same time need one each.
  *   - dtype: ROLLOUT_DTYPE_F32, _BF16 or _F16.  Strides count elements between rows; inside a row values are consecutive.
- *     Rows need only be aligned to their elements.
+ *     Rows need only be aligned to their elements (rollout_head_*: to 16 bytes).
  *   - Sums are fp32, taken in an order that the sizes fix: the same inputs give the same bits.
  *   - Errors: E_INVAL, E_HIP; rollout_last_error(NULL) gives the text. */
 
@@ -408,6 +408,25 @@ int64_t rollout_embed_grad_workspace(int32_t n, int32_t vocab, int32_t hidden);
 int rollout_embed_grad(const void *grad_rows, int32_t dtype, int32_t n, int32_t vocab, int32_t hidden, int64_t row_stride,
                        const int32_t *tokens, float scale, const void *base, int32_t table_dtype, void *workspace,
                        size_t workspace_bytes, void *hip_stream, void *grad_table);
+
+/* rollout_token_logprobs of the logits x = hidden_states . lm_head^T, which never reach memory: bf16 hidden_states
+ * [rows][hidden] and lm_head [vocab][hidden], products summed in fp32.  hidden a multiple of 32, rows of both arrays
+ * aligned to 16 bytes. */
+int64_t rollout_head_logprobs_workspace(int32_t rows, int32_t vocab, int32_t hidden);
+int rollout_head_logprobs(const void *hidden_states, int64_t hidden_stride, const void *lm_head, int64_t head_stride,
+                          int32_t rows, int32_t vocab, int32_t hidden, float temperature, const int32_t *targets,
+                          void *workspace, size_t workspace_bytes, void *hip_stream, float *logp, float *entropy,
+                          float *row_stats);
+
+/* Its gradients with respect to hidden_states and lm_head, from the logits' gradient g as in rollout_token_logprobs_grad
+ * (rounded to bf16 for the products): grad_hidden = g . lm_head [rows][hidden], grad_head = g^T . hidden_states
+ * [vocab][hidden], both bf16 without gaps.  Rows whose gradients are both 0 take no part: their grad_hidden is 0. */
+int64_t rollout_head_logprobs_grad_workspace(int32_t rows, int32_t vocab, int32_t hidden);
+int rollout_head_logprobs_grad(const void *hidden_states, int64_t hidden_stride, const void *lm_head, int64_t head_stride,
+                               int32_t rows, int32_t vocab, int32_t hidden, float temperature, const int32_t *targets,
+                               const float *row_stats, const float *entropy, const float *grad_logp,
+                               const float *grad_entropy, void *workspace, size_t workspace_bytes, void *hip_stream,
+                               void *grad_hidden, void *grad_head);
 
 /* Parity hook: copies the fp32 logits rows of the last prefill (one per prompt, prompt
  * order) or decode step (one per stepped sample, ascending id) to host `out`

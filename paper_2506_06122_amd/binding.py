@@ -135,6 +135,12 @@ SIGNATURES = {
     "rollout_embed_grad_workspace": (C.c_int64, [C.c_int32] * 3),
     "rollout_embed_grad": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, _P, C.c_float, _P,
                                      C.c_int32, _P, C.c_size_t, _P, _P]),
+    "rollout_head_logprobs_workspace": (C.c_int64, [C.c_int32] * 3),
+    "rollout_head_logprobs": (C.c_int, [_P, C.c_int64, _P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, _P, _P,
+                                        C.c_size_t, _P, _P, _P, _P]),
+    "rollout_head_logprobs_grad_workspace": (C.c_int64, [C.c_int32] * 3),
+    "rollout_head_logprobs_grad": (C.c_int, [_P, C.c_int64, _P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_float, _P,
+                                             _P, _P, _P, _P, _P, C.c_size_t, _P, _P, _P]),
     "rollout_pool_create": (_P, [C.c_int32]),
     "rollout_pool_destroy": (None, [_P]),
     "rollout_pool_free_pages": (C.c_int32, [_P]),
@@ -655,6 +661,58 @@ def rollout_embed_grad(grad_rows, tokens, vocab, *, scale=1.0, base=None, dtype=
                                               base.data_ptr() if base is not None else None, _dtype_id(out, "out"),
                                               ws.data_ptr(), len(ws), s, out.data_ptr()))
     return out
+
+
+def _head(hidden_states, lm_head, targets):
+    import torch
+    device = hidden_states.device
+    rows, hidden = hidden_states.shape if hidden_states.dim() == 2 else (0, 0)
+    stride = _rows(hidden_states, "hidden_states", device, torch.bfloat16)
+    head_stride = _rows(lm_head, "lm_head", device, torch.bfloat16)
+    vocab = len(lm_head)
+    if lm_head.shape[1] != hidden:
+        _refuse("lm_head must have as many columns as hidden_states")
+    tgt = _vector(targets, "targets", device, torch.int32, rows)
+    return device, rows, vocab, hidden, (hidden_states.data_ptr(), stride, lm_head.data_ptr(), head_stride, rows, vocab, hidden), tgt
+
+
+def rollout_head_logprobs(hidden_states, lm_head, targets=None, *, temperature=1.0, stream=None):
+    """rollout_token_logprobs of the logits hidden_states . lm_head^T without storing them: bfloat16 CUDA tensors
+    [rows][hidden] and [vocab][hidden], hidden a multiple of 32.  Returns (logp, entropy, row_stats).  Stream as in
+    rollout_token_logprobs."""
+    import torch
+    lib = load_library()
+    device, rows, vocab, hidden, args, tgt = _head(hidden_states, lm_head, targets)
+    with _On(device, stream) as s:
+        ws = _workspace(lib, lib.rollout_head_logprobs_workspace(rows, vocab, hidden), device)
+        logp, entropy = torch.empty(rows, device=device), torch.empty(rows, device=device)
+        stats = torch.empty(rows, 2, device=device)
+        _enqueued(lib, lib.rollout_head_logprobs(*args, temperature, tgt, ws.data_ptr() if ws is not None else None,
+                                                 len(ws) if ws is not None else 0, s, logp.data_ptr(), entropy.data_ptr(),
+                                                 stats.data_ptr()))
+    return logp, entropy, stats
+
+
+def rollout_head_logprobs_grad(hidden_states, lm_head, targets, row_stats, entropy, grad_logp, grad_entropy=None, *,
+                               temperature=1.0, stream=None):
+    """(grad_hidden [rows][hidden], grad_head [vocab][hidden]), bfloat16, from the gradients of rollout_head_logprobs' logp
+    and (or None) entropy; row_stats and entropy are what it returned.  Stream as in rollout_token_logprobs."""
+    import torch
+    lib = load_library()
+    device, rows, vocab, hidden, args, tgt = _head(hidden_states, lm_head, targets)
+    if _rows(row_stats, "row_stats", device, torch.float32, (rows, 2)) != 2:
+        _refuse("row_stats must be contiguous")
+    ent = _vector(entropy, "entropy", device, torch.float32, rows)
+    gl = _vector(grad_logp, "grad_logp", device, torch.float32, rows)
+    ge = _vector(grad_entropy, "grad_entropy", device, torch.float32, rows)
+    with _On(device, stream) as s:
+        ws = _workspace(lib, lib.rollout_head_logprobs_grad_workspace(rows, vocab, hidden), device)
+        grad_hidden = torch.empty(rows, hidden, dtype=torch.bfloat16, device=device)
+        grad_head = torch.empty(vocab, hidden, dtype=torch.bfloat16, device=device)
+        _enqueued(lib, lib.rollout_head_logprobs_grad(*args, temperature, tgt, row_stats.data_ptr(), ent, gl, ge,
+                                                      ws.data_ptr(), len(ws), s, grad_hidden.data_ptr(),
+                                                      grad_head.data_ptr()))
+    return grad_hidden, grad_head
 
 
 def rollout_philox_words(seed, sample_ids, steps):

@@ -27,10 +27,14 @@ void check_array(const void* p, size_t align, const char* name) {
 void check_optional(const void* p, size_t align, const char* name) {
   if (p) check_array(p, align, name);
 }
-void check_stride(int64_t stride, int width, int64_t multiple, const char* name) {
-  if (stride < width || stride > (int64_t)1 << 40 || stride % multiple)
-    fail(ROLLOUT_E_INVAL, std::string(name) + " must be at least the row's length" +
-                              (multiple > 1 ? " and a multiple of " + std::to_string(multiple) : ""));
+constexpr int64_t kMaxStride = (int64_t)1 << 40;
+void check_stride(int64_t stride, int width, const char* name) {
+  if (stride < width || stride > kMaxStride) fail(ROLLOUT_E_INVAL, std::string(name) + " must be at least the row's length");
+}
+// operands of matrix products: 256 rows are reached by a 32-bit offset in bytes
+void check_operand_stride(int64_t stride, int width, const char* name) {
+  if (stride < width || stride > (int64_t)1 << 22 || stride % 8)
+    fail(ROLLOUT_E_INVAL, std::string(name) + " must be a multiple of 8 from the row's length to 2^22");
 }
 float inverse(float temperature) {
   const float inv = 1.0f / temperature;
@@ -73,6 +77,18 @@ void check_gradients(const float* row_stats, const float* entropy, const float* 
   if (grad_entropy) check_array(entropy, 4, "entropy");
 }
 
+HeadArgs head_args(const void* hidden_states, int64_t hidden_stride, const void* lm_head, int64_t head_stride, int rows,
+                   int vocab, int hidden, float temperature, const int32_t* targets) {
+  check_sizes(rows, vocab, hidden);
+  if (hidden % 32) fail(ROLLOUT_E_INVAL, "hidden must be a multiple of 32");
+  check_operand_stride(hidden_stride, hidden, "hidden_stride");
+  check_operand_stride(head_stride, hidden, "head_stride");
+  check_optional(targets, 4, "targets");
+  check_array(lm_head, 16, "lm_head");
+  if (rows > 0) check_array(hidden_states, 16, "hidden_states");
+  return HeadArgs{hidden_states, hidden_stride, lm_head, head_stride, rows, vocab, hidden, inverse(temperature), targets};
+}
+
 }  // namespace
 
 extern "C" {
@@ -93,7 +109,7 @@ int rollout_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int3
     check_sizes(rows, vocab, 1);
     check_dtype(dtype);
     check_top(top, vocab);
-    check_stride(row_stride, vocab, 1, "row_stride");
+    check_stride(row_stride, vocab, "row_stride");
     const float inv_temp = inverse(temperature);
     if (rows == 0) return;
     check_array(logits, vt_size(dtype), "logits");
@@ -119,8 +135,8 @@ int rollout_token_logprobs_grad(const void* logits, int32_t dtype, int32_t rows,
   return guarded(nullptr, [&] {
     check_sizes(rows, vocab, 1);
     check_dtype(dtype);
-    check_stride(row_stride, vocab, 1, "row_stride");
-    check_stride(grad_row_stride, vocab, 1, "grad_row_stride");
+    check_stride(row_stride, vocab, "row_stride");
+    check_stride(grad_row_stride, vocab, "grad_row_stride");
     const float inv_temp = inverse(temperature);
     if (rows == 0) return;
     check_array(logits, vt_size(dtype), "logits");
@@ -140,7 +156,7 @@ int rollout_embed(const void* table, int32_t dtype, int32_t vocab, int32_t hidde
   return guarded(nullptr, [&] {
     check_sizes(n, vocab, hidden);
     check_dtype(dtype);
-    check_stride(table_stride, hidden, 1, "table_stride");
+    check_stride(table_stride, hidden, "table_stride");
     check_scale(scale);
     if (n == 0) return;
     check_array(table, vt_size(dtype), "table");
@@ -165,7 +181,7 @@ int rollout_embed_grad(const void* grad_rows, int32_t dtype, int32_t n, int32_t 
     check_sizes(n, vocab, hidden);
     check_dtype(dtype);
     if (table_dtype != dtype && table_dtype != VT_F32) fail(ROLLOUT_E_INVAL, "table_dtype must be dtype or ROLLOUT_DTYPE_F32");
-    check_stride(row_stride, hidden, 1, "row_stride");
+    check_stride(row_stride, hidden, "row_stride");
     check_scale(scale);
     if (n > 0) {
       check_array(grad_rows, vt_size(dtype), "grad_rows");
@@ -176,6 +192,54 @@ int rollout_embed_grad(const void* grad_rows, int32_t dtype, int32_t n, int32_t 
     check_workspace(workspace, workspace_bytes, embed_grad_workspace(n, vocab, hidden));
     const EmbedGrad a{grad_rows, row_stride, dtype, tokens, n, vocab, hidden, scale, base, table_dtype, grad_table};
     enqueue([&] { launch_embed_grad(a, workspace, (hipStream_t)hip_stream); });
+  });
+}
+
+int64_t rollout_head_logprobs_workspace(int32_t rows, int32_t vocab, int32_t hidden) {
+  return bytes_of([&] {
+    check_sizes(rows, vocab, hidden);
+    return head_workspace(rows, vocab, hidden);
+  });
+}
+
+int rollout_head_logprobs(const void* hidden_states, int64_t hidden_stride, const void* lm_head, int64_t head_stride,
+                          int32_t rows, int32_t vocab, int32_t hidden, float temperature, const int32_t* targets,
+                          void* workspace, size_t workspace_bytes, void* hip_stream, float* logp, float* entropy,
+                          float* row_stats) {
+  return guarded(nullptr, [&] {
+    const HeadArgs in = head_args(hidden_states, hidden_stride, lm_head, head_stride, rows, vocab, hidden, temperature, targets);
+    if (rows == 0) return;
+    check_array(logp, 4, "logp");
+    check_array(entropy, 4, "entropy");
+    check_array(row_stats, 4, "row_stats");
+    check_workspace(workspace, workspace_bytes, head_workspace(rows, vocab, hidden));
+    const TokenOut out{logp, entropy, row_stats, 0, nullptr, nullptr};
+    enqueue([&] { launch_head_logprobs(in, out, workspace, (hipStream_t)hip_stream); });
+  });
+}
+
+int64_t rollout_head_logprobs_grad_workspace(int32_t rows, int32_t vocab, int32_t hidden) {
+  return bytes_of([&] {
+    check_sizes(rows, vocab, hidden);
+    return head_grad_workspace(rows, vocab, hidden);
+  });
+}
+
+int rollout_head_logprobs_grad(const void* hidden_states, int64_t hidden_stride, const void* lm_head, int64_t head_stride,
+                               int32_t rows, int32_t vocab, int32_t hidden, float temperature, const int32_t* targets,
+                               const float* row_stats, const float* entropy, const float* grad_logp,
+                               const float* grad_entropy, void* workspace, size_t workspace_bytes, void* hip_stream,
+                               void* grad_hidden, void* grad_head) {
+  return guarded(nullptr, [&] {
+    const HeadArgs in = head_args(hidden_states, hidden_stride, lm_head, head_stride, rows, vocab, hidden, temperature, targets);
+    check_array(grad_head, 16, "grad_head");
+    if (rows > 0) {
+      check_array(grad_hidden, 16, "grad_hidden");
+      check_gradients(row_stats, entropy, grad_logp, grad_entropy);
+    }
+    check_workspace(workspace, workspace_bytes, head_grad_workspace(rows, vocab, hidden));
+    const HeadGrad a{in, row_stats, entropy, grad_logp, grad_entropy, grad_hidden, grad_head};
+    enqueue([&] { launch_head_logprobs_grad(a, workspace, (hipStream_t)hip_stream); });
   });
 }
 

@@ -1,0 +1,520 @@
+// Log-probs of given tokens straight from hidden states and the lm_head matrix, and the gradients of both.
+//
+//   x = h W^T (never stored);  sums of every row as in kernels_vocab.hip
+//   g = the logits' gradient;  dh = g W;  dW = g^T h
+//
+// Three products of 2 R H V operations each, one of them twice (the gradient needs the logits again), so matrix-core
+// bound for more than a few rows; with a few the walk over W is.  One kernel does all of them: C = A B^T over tiles, where
+// each operand lies with its rows or with the summed index outermost, as the caller or the previous launch left it -
+// fragments of the second kind are transposed on their way out of LDS - so that nothing is transposed in memory.
+#include "vocab.h"
+
+#include <algorithm>
+#include <utility>
+
+#include "head_tile.h"
+#include "vocab_vec.h"
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// What becomes of a tile of C
+//   TO_SUMS   the logits of a row over the tile's columns become one RowSums; the target's logit is stored
+//   TO_GRAD   logits become their gradients, bf16
+//   TO_PLANE  fp32, one plane per split of K; with `add` on top of what is there
+//   TO_BF16   bf16
+enum { TO_SUMS, TO_GRAD, TO_PLANE, TO_BF16 };
+
+struct Operand {
+  const void* p;
+  long long pitch;  // elements between rows, or with the summed index outermost between its steps
+};
+struct Product {
+  Operand a, b;
+  int M, N, K;          // b with K outermost has exactly K steps; anything else is padded to whole k-tiles
+  const int* count;     // device: where not NULL, M (or K, with `count_is_k`) is *count
+  bool count_is_k;
+  int splits, k_tiles_per_split;
+  int m_tiles, n_tiles; // of the grid
+  void* out;
+  long long out_pitch;
+  bool add;
+  float inv_temp;
+  // TO_SUMS
+  const int* targets;
+  RowSums* sums;        // [M][n_tiles]
+  float* target_logit;  // [M]
+  // TO_GRAD: rows of A are rows active[.] of the caller's arrays; columns start at col0 of the vocabulary
+  const int* active;
+  const float *row_stats, *entropy, *grad_logp, *grad_entropy;
+  int col0, vocab, row_capacity;
+};
+
+__device__ __forceinline__ void load_to_lds(unsigned lds, unsigned voff, const void* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base)
+               : "memory");
+}
+// this wavefront's loads but the last N have arrived and its LDS reads are done; then the barrier
+template <int N>
+__device__ __forceinline__ void wait_and_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+template <class F, int... I>
+__device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// Fragment i of a slice in LDS
+template <int C, bool KM>
+__device__ __forceinline__ u32x4 fragment(const char* slice, int i, int lane) {
+  const char* p = slice + HeadSlice<C, KM>::fragment(i, lane);
+  if constexpr (KM) {
+    typedef __attribute__((address_space(3))) s16x4* lds_t;
+    struct Two {
+      s16x4 a, b;
+    } v;
+    v.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)p);
+    v.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(p + 4 * HeadSlice<C, KM>::pitch));
+    return __builtin_bit_cast(u32x4, v);
+  } else {
+    return *(const u32x4*)p;
+  }
+}
+
+// A workgroup computes BM = 16 WM MT rows x BN = 16 WN NT columns of C; its WM x WN wavefronts own MT x NT tiles of 16 x 16
+// each.  Slices of 32 steps of K go straight from memory into a ring of S LDS stages; the fragments of stage s + 1 are read,
+// and the copies of stage s + S issued, between the products of stage s, with one barrier per stage: it says that every
+// wavefront's copies of stage s + 1 have arrived (loads are counted in order, later stages stay in flight) and that
+// everyone holds stage s in registers.  The copies past the end of K repeat the last slice, so that every stage counts
+// the same number of them.
+template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
+__global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_product_kernel(Product p) {
+  constexpr bool WIDE = MT * NT >= 32;
+  constexpr int NW = WM * WN, BM = WM * MT * 16, BN = WN * NT * 16;
+  using A = HeadSlice<BM, AK>;
+  using B = HeadSlice<BN, BK>;
+  constexpr int U = A::units + B::units, L = (U + NW - 1) / NW, STAGE = U * 1024;
+  static_assert(S * STAGE <= 160 * 1024 && S >= 2 && (S - 1) * L < 64, "fits the CU and the load counter");
+  __shared__ __attribute__((aligned(1024))) char lds[S * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const HeadBlock block = head_block(blockIdx.x, p.m_tiles, p.n_tiles, p.splits);
+  if (!block.inside) return;
+  const int bn = block.n, bz = block.z;
+  const int M = p.count && !p.count_is_k ? *p.count : p.M, K = p.count && p.count_is_k ? *p.count : p.K;
+  const int m0 = block.m * BM, n0 = bn * BN;
+  const HeadExtent x = head_extent(AK, BK, TO == TO_GRAD, m0, n0, bz, M, p.N, K, p.k_tiles_per_split, p.a.pitch, p.row_capacity);
+  if (m0 >= x.m_end) return;
+  const int k_tiles = x.k_tiles, kt_begin = x.kt_begin, kt_end = x.kt_end;
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int wm = wave / WN, wn = wave % WN;
+  if (kt_begin < kt_end) {
+    // this wavefront's loads of a stage: units wave, wave + NW, ... of A's, then B's; their sources move on with the slices
+    unsigned voff[L], tail[L], dst[L];
+    bool is_b[L];
+    const long long a_step = AK ? p.a.pitch * 64 : 64, b_step = BK ? p.b.pitch * 64 : 64;
+    const char* pa = (const char*)p.a.p + 2 * (AK ? m0 : m0 * p.a.pitch) + kt_begin * a_step;
+    const char* pb = (const char*)p.b.p + 2 * (BK ? n0 : n0 * p.b.pitch) + kt_begin * b_step;
+#pragma unroll
+    for (int s = 0; s < L; ++s) {
+      const int u = __builtin_amdgcn_readfirstlane(min(s * NW + wave, U - 1));  // an uneven last round loads the last one again
+      is_b[s] = u >= A::units;
+      dst[s] = u * 1024;
+      if (!is_b[s]) {
+        tail[s] = voff[s] = (unsigned)A::source(u, lane, x.a_limit, 32, p.a.pitch);
+      } else {
+        voff[s] = (unsigned)B::source(u - A::units, lane, x.b_limit, 32, p.b.pitch);
+        tail[s] = BK ? (unsigned)B::source(u - A::units, lane, x.b_limit, x.b_last, p.b.pitch) : voff[s];
+      }
+    }
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds;
+    int ahead = kt_begin;  // k-tile of the next copies
+    auto issue = [&](int s, int buf) __attribute__((always_inline)) {
+      const unsigned to = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + dst[s]);
+      const unsigned from = BK && ahead == k_tiles - 1 ? tail[s] : voff[s];
+      load_to_lds(to, from, is_b[s] ? pb : pa);
+    };
+    auto move_on = [&]() __attribute__((always_inline)) {
+      if (ahead + 1 < kt_end) {
+        ++ahead;
+        pa += a_step;
+        pb += b_step;
+      }
+    };
+#pragma unroll
+    for (int q = 0; q < S; ++q) {
+#pragma unroll
+      for (int s = 0; s < L; ++s) issue(s, q);
+      move_on();
+    }
+    u32x4 a[2][MT], b[2][NT];
+    constexpr int NR = MT + NT, NM = MT * NT, NS = NR + L;
+    auto read = [&](int y, const char* st, int f) __attribute__((always_inline)) {  // in the order in which they are multiplied
+      if (f < 1) a[y][0] = fragment<BM, AK>(st, wm * MT, lane);
+      else if (f < 1 + NT) b[y][f - 1] = fragment<BN, BK>(st + A::units * 1024, wn * NT + f - 1, lane);
+      else a[y][f - NT] = fragment<BM, AK>(st, wm * MT + f - NT, lane);
+    };
+    auto mul = [&](int y, int q) __attribute__((always_inline)) {
+      const int i = q / NT, j = q % NT;
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[y][j]),
+                                                          __builtin_bit_cast(bf16x8, a[y][i]), acc[i][j], 0, 0, 0);
+    };
+    auto keep_sums = [&]() __attribute__((always_inline)) {  // in the accumulation registers at the end of each stage
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) asm volatile("" : "+a"(acc[i][j]));
+      }
+    };
+    keep_sums();
+    wait_and_barrier<(S - 1) * L>();
+#pragma unroll
+    for (int f = 0; f < NR; ++f) read(0, lds, f);
+    int buf = 0;
+    auto stage = [&](int y) __attribute__((always_inline)) {
+      wait_and_barrier<(S - 2) * L>();
+      const int next = buf == S - 1 ? 0 : buf + 1;
+      const char* st = lds + next * STAGE;
+      unrolled([&](auto qc) __attribute__((always_inline)) {
+        constexpr int q = decltype(qc)::value, u0 = (q * NS + NM - 1) / NM, u1 = ((q + 1) * NS + NM - 1) / NM;
+        mul(y, q);
+#pragma unroll
+        for (int u = u0; u < u1; ++u) {
+          if (u < NR) read(y ^ 1, st, u);
+          else issue(u - NR, buf);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }, std::make_integer_sequence<int, NM>{});
+      move_on();
+      keep_sums();
+      buf = next;
+    };
+    auto last = [&](int y) __attribute__((always_inline)) {
+      unrolled([&](auto qc) __attribute__((always_inline)) { mul(y, decltype(qc)::value); }, std::make_integer_sequence<int, NM>{});
+      keep_sums();
+    };
+    int left = kt_end - kt_begin;
+    for (; left > 2; left -= 2) {
+      stage(0);
+      stage(1);
+    }
+    if (left == 2) {
+      stage(0);
+      last(1);
+    } else {
+      last(0);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may still be on its way into LDS
+  }
+  // acc[i][j][e]: row 16 (wm MT + i) + r, column 16 (wn NT + j) + 4 g + e of the tile
+  const int col = n0 + wn * NT * 16 + 4 * g;
+
+  if constexpr (TO == TO_SUMS) {
+    const float c = p.inv_temp * kLog2e;
+    __syncthreads();
+    RowSums* part = (RowSums*)lds;  // [WN][BM]
+    const bool whole = n0 + BN <= p.N;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int ml = (wm * MT + i) * 16 + r, m = m0 + ml;
+      // the target's place among this lane's values, if it is one of them: 4 j + e
+      const int target = p.targets && m < M ? p.targets[m] : -1;
+      const int from = target - (n0 + wn * NT * 16), place = (from >> 4) * 4 + (from & 3);
+      const bool here = target >= 0 && target < p.N && from >= 0 && from < NT * 16 && (from >> 2 & 3) == g;
+      float x_target = 0.f;
+      RowSums s{-3.402823466e38f, 0.f, 0.f};
+      if (!whole) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (col + j * 16 + e >= p.N) acc[i][j][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x_target = place == 4 * j + e ? acc[i][j][e] : x_target;
+          s.m = fmaxf(s.m, acc[i][j][e]);
+        }
+      if (here) p.target_logit[m] = x_target;
+      s.m = fmaxf(s.m, __shfl_xor(s.m, 16, WAVE));
+      s.m = fmaxf(s.m, __shfl_xor(s.m, 32, WAVE));
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float y = (acc[i][j][e] - s.m) * c, w = __builtin_amdgcn_exp2f(y);
+          s.s += w;
+          s.t = fmaf(w, fmaxf(y, -1e30f), s.t);
+        }
+      s.s += __shfl_xor(s.s, 16, WAVE);
+      s.s += __shfl_xor(s.s, 32, WAVE);
+      s.t += __shfl_xor(s.t, 16, WAVE);
+      s.t += __shfl_xor(s.t, 32, WAVE);
+      if (g == 0) part[wn * BM + ml] = s;
+    }
+    __syncthreads();
+    for (int ml = threadIdx.x; ml < BM && m0 + ml < M; ml += NW * 64) {
+      RowSums s = part[ml];
+#pragma unroll
+      for (int w = 1; w < WN; ++w) s = merge(s, part[w * BM + ml], c);
+      p.sums[(long long)(m0 + ml) * p.n_tiles + bn] = s;
+    }
+  } else if constexpr (TO == TO_GRAD) {
+    const float c = p.inv_temp * kLog2e;
+    __syncthreads();
+    RowGrad* rows = (RowGrad*)lds;
+    for (int ml = threadIdx.x; ml < BM; ml += NW * 64) {
+      RowGrad q{};
+      q.none = true;
+      if (m0 + ml < M)
+        q = row_grad(p.row_stats, p.entropy, p.grad_logp, p.grad_entropy, p.targets, p.inv_temp, p.vocab, p.active[m0 + ml]);
+      rows[ml] = q;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int ml = (wm * MT + i) * 16 + r, m = m0 + ml;
+      const RowGrad q = rows[ml];
+      if (m < x.m_end) {
+        const int target = q.target - p.col0;
+        uint16_t* o = (uint16_t*)p.out + m * p.out_pitch;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const int n = col + j * 16;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = grad_of(acc[i][j][e], c, q);
+            if (n + e == target && q.target >= 0) v[e] += q.at_target;
+            if (q.none || n + e >= p.N) v[e] = 0.f;
+          }
+          if (n < p.out_pitch) {  // columns up to the pitch are the padding of K in the product that follows
+            uint2 w;
+            w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{v[0], v[1]}), bf16_pair));
+            w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{v[2], v[3]}), bf16_pair));
+            *(uint2*)(o + n) = w;
+          }
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int m = m0 + (wm * MT + i) * 16 + r;
+      if (m < M) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const int n = col + j * 16;
+          if (n < p.N) {  // N is a multiple of 32
+            if constexpr (TO == TO_PLANE) {
+              f32x4* o = (f32x4*)((float*)p.out + ((long long)bz * p.M + m) * p.out_pitch + n);
+              *o = p.add ? *o + acc[i][j] : acc[i][j];
+            } else {
+              uint2 w;
+              w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][0], acc[i][j][1]}), bf16_pair));
+              w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][2], acc[i][j][3]}), bf16_pair));
+              *(uint2*)((uint16_t*)p.out + m * p.out_pitch + n) = w;
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
+// ---- a row's parts -> its results: one wavefront per row --------------------------------------
+__global__ __launch_bounds__(256) void head_finish_kernel(HeadArgs in, TokenOut out, const RowSums* sums, const float* target_logit, int parts) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= in.rows) return;
+  const float c = in.inv_temp * kLog2e;
+  RowSums s{-3.402823466e38f, 0.f, 0.f};
+  for (int i = lane; i < parts; i += WAVE) s = merge(s, sums[(long long)row * parts + i], c);
+#pragma unroll
+  for (int o = 1; o < WAVE; o <<= 1) s = merge(s, RowSums{__shfl_xor(s.m, o, WAVE), __shfl_xor(s.s, o, WAVE), __shfl_xor(s.t, o, WAVE)}, c);
+  if (lane) return;
+  const int t = in.targets ? in.targets[row] : -1;
+  const bool has = t >= 0 && t < in.vocab;
+  finish_row(s, out, row, has, has ? target_logit[row] : 0.f, in.inv_temp);
+}
+
+// ---- rows that have a gradient ---------------------------------------------------------------
+// active[i] = i-th row with a gradient, place[row] = its i or -1, *count = their number.  One workgroup.
+__global__ __launch_bounds__(1024) void head_active_kernel(HeadGrad a, int* count, int* active, int* place) {
+  __shared__ int wave_s[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int done = 0;
+  for (int r0 = 0; r0 < a.in.rows; r0 += 1024) {
+    const int r = r0 + tid;
+    bool has = false;
+    if (r < a.in.rows)
+      has = !row_grad(a.row_stats, a.entropy, a.grad_logp, a.grad_entropy, a.in.targets, a.in.inv_temp, a.in.vocab, r).none;
+    const unsigned long long mask = __ballot(has);
+    if (lane == 0) wave_s[wave] = __popcll(mask);
+    __syncthreads();
+    int at = done, all = 0;
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) at += wave_s[w];
+      all += wave_s[w];
+    }
+    at += __popcll(mask & ((1ull << lane) - 1));
+    if (r < a.in.rows) place[r] = has ? at : -1;
+    if (has) active[at] = r;
+    done += all;
+    __syncthreads();
+  }
+  if (tid == 0) *count = done;
+}
+// out[i] = hidden_states[active[i]], zeros behind them up to a whole k-tile; one row per workgroup
+__global__ __launch_bounds__(256) void head_gather_kernel(HeadArgs in, const int* count, const int* active, uint16_t* out) {
+  const int i = blockIdx.x, n = *count;
+  if (i >= ((n + 31) & ~31)) return;
+  const u32x4* src = i < n ? (const u32x4*)((const uint16_t*)in.hidden_states + active[i] * in.hidden_stride) : nullptr;
+  u32x4* dst = (u32x4*)(out + (long long)i * in.hidden);
+  const u32x4 zero = {0, 0, 0, 0};
+  for (int v = threadIdx.x; v < in.hidden / 8; v += 256) dst[v] = src ? src[v] : zero;
+}
+// grad_hidden[row] = sum of the planes' row place[row], in their order; zeros where the row has none
+__global__ __launch_bounds__(256) void head_planes_kernel(const float* planes, int splits, int rows, int hidden, const int* place, uint16_t* out) {
+  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int per_row = hidden / 4, row = (int)(at / per_row), col = (int)(at % per_row) * 4;
+  if (row >= rows) return;
+  const int i = place[row];
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (i >= 0)
+    for (int z = 0; z < splits; ++z) s += *(const f32x4*)(planes + ((long long)z * rows + i) * hidden + col);
+  uint2 w;
+  w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{s[0], s[1]}), bf16_pair));
+  w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{s[2], s[3]}), bf16_pair));
+  *(uint2*)(out + (long long)row * hidden + col) = w;
+}
+
+// ---- shapes ------------------------------------------------------------------------------------
+template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
+void launch_shape(Product p, hipStream_t s) {
+  p.m_tiles = head_ceil(TO == TO_GRAD ? p.row_capacity : p.M, WM * MT * 16);
+  p.n_tiles = head_ceil(p.N, WN * NT * 16);
+  p.k_tiles_per_split = head_ceil(head_ceil(p.K, 32), p.splits);
+  head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK><<<head_blocks(p.m_tiles * p.n_tiles * p.splits), WM * WN * 64, 0, s>>>(p);
+}
+template <int TO, bool AK, bool BK>
+void launch_product(const Product& p, hipStream_t s) {
+  const HeadTile t = head_tile(p.M, p.N);
+  if (t.m == 16) launch_shape<1, 4, 1, 4, 4, TO, AK, BK>(p, s);
+  else if (t.m == 32) launch_shape<1, 4, 2, 4, 4, TO, AK, BK>(p, s);
+  else if (t.m == 64) launch_shape<1, 4, 4, 4, 4, TO, AK, BK>(p, s);
+  else if (t.m == 128) launch_shape<2, 2, 4, 4, 4, TO, AK, BK>(p, s);
+  else launch_shape<2, 2, 8, 8, 4, TO, AK, BK>(p, s);
+}
+
+constexpr size_t piece(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+}  // namespace
+
+size_t head_workspace(int rows, int vocab, int) {
+  const HeadTile t = head_tile(rows, vocab);
+  return piece((size_t)rows * 4) + (size_t)rows * ceil_div(vocab, t.n) * sizeof(RowSums);
+}
+void launch_head_logprobs(const HeadArgs& in, const TokenOut& out, void* ws, hipStream_t s) {
+  Product p{};
+  p.a = {in.hidden_states, in.hidden_stride};
+  p.b = {in.lm_head, in.head_stride};
+  p.M = in.rows;
+  p.N = in.vocab;
+  p.K = in.hidden;
+  p.splits = 1;
+  p.inv_temp = in.inv_temp;
+  p.targets = in.targets;
+  p.target_logit = (float*)ws;
+  p.sums = (RowSums*)((char*)ws + piece((size_t)in.rows * 4));
+  launch_product<TO_SUMS, false, false>(p, s);
+  head_finish_kernel<<<ceil_div(in.rows, 4), 256, 0, s>>>(in, out, p.sums, p.target_logit, ceil_div(in.vocab, head_tile(in.rows, in.vocab).n));
+}
+
+size_t head_grad_workspace(int rows, int vocab, int hidden) {
+  const HeadGradPlan g = head_grad_plan(rows, vocab, hidden);
+  return piece(4) + 2 * piece((size_t)rows * 4) + piece((size_t)g.rows * hidden * 2) + piece((size_t)g.rows * g.chunk * 2) +
+         piece((size_t)g.splits * rows * hidden * 4);
+}
+void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
+  const HeadArgs& in = a.in;
+  const HeadGradPlan g = head_grad_plan(in.rows, in.vocab, in.hidden);
+  char* at = (char*)ws;
+  auto take = [&](size_t bytes) {
+    void* r = at;
+    at += piece(bytes);
+    return r;
+  };
+  int* count = (int*)take(4);
+  int* active = (int*)take((size_t)in.rows * 4);
+  int* place = (int*)take((size_t)in.rows * 4);
+  uint16_t* h = (uint16_t*)take((size_t)g.rows * in.hidden * 2);
+  uint16_t* dx = (uint16_t*)take((size_t)g.rows * g.chunk * 2);
+  float* planes = (float*)take((size_t)g.splits * in.rows * in.hidden * 4);
+  head_active_kernel<<<1, 1024, 0, s>>>(a, count, active, place);
+  head_gather_kernel<<<g.rows, 256, 0, s>>>(in, count, active, h);
+  for (int v0 = 0; v0 < in.vocab; v0 += g.chunk) {
+    const int v = std::min(g.chunk, in.vocab - v0);
+    const uint16_t* w = (const uint16_t*)in.lm_head + v0 * in.head_stride;
+    if (in.rows > 0) {
+      Product p{};  // logits of the chunk and their gradients
+      p.a = {h, in.hidden};
+      p.b = {w, in.head_stride};
+      p.M = in.rows;
+      p.N = v;
+      p.K = in.hidden;
+      p.count = count;
+      p.splits = 1;
+      p.out = dx;
+      p.out_pitch = head_grad_pitch(v);
+      p.inv_temp = in.inv_temp;
+      p.targets = in.targets;
+      p.active = active;
+      p.row_stats = a.row_stats;
+      p.entropy = a.entropy;
+      p.grad_logp = a.grad_logp;
+      p.grad_entropy = a.grad_entropy;
+      p.col0 = v0;
+      p.vocab = in.vocab;
+      p.row_capacity = g.rows;
+      launch_product<TO_GRAD, false, false>(p, s);
+      Product q{};  // + dx W
+      q.a = {dx, p.out_pitch};
+      q.b = {w, in.head_stride};
+      q.M = in.rows;
+      q.N = in.hidden;
+      q.K = v;
+      q.count = count;
+      q.splits = std::min(g.splits, std::max(1, ceil_div(v, 32)));
+      q.out = planes;
+      q.out_pitch = in.hidden;
+      q.add = v0 > 0;
+      launch_product<TO_PLANE, false, true>(q, s);
+    }
+    Product q{};  // dx^T h
+    q.a = {dx, head_grad_pitch(v)};
+    q.b = {h, in.hidden};
+    q.M = v;
+    q.N = in.hidden;
+    q.K = g.rows;
+    q.count = count;
+    q.count_is_k = true;
+    q.splits = 1;
+    q.out = (uint16_t*)a.grad_head + (long long)v0 * in.hidden;
+    q.out_pitch = in.hidden;
+    launch_product<TO_BF16, true, true>(q, s);
+  }
+  if (in.rows > 0)
+    head_planes_kernel<<<ceil_div((long long)in.rows * (in.hidden / 4), 256), 256, 0, s>>>(planes, g.splits, in.rows, in.hidden, place,
+                                                                                    (uint16_t*)a.grad_hidden);
+}

@@ -119,3 +119,25 @@ struct EmbedGrad {
 };
 size_t embed_grad_workspace(int n, int vocab, int hidden);
 void launch_embed_grad(const EmbedGrad& a, void* workspace, hipStream_t s);
+
+// ---- lm_head -----------------------------------------------------------------------------
+struct HeadArgs {
+  const void* hidden_states;  // bf16 [rows][hidden]
+  long long hidden_stride;
+  const void* lm_head;        // bf16 [vocab][hidden]
+  long long head_stride;
+  int rows, vocab, hidden;
+  float inv_temp;
+  const int* targets;
+};
+size_t head_workspace(int rows, int vocab, int hidden);
+void launch_head_logprobs(const HeadArgs& in, const TokenOut& out, void* workspace, hipStream_t s);
+
+struct HeadGrad {
+  HeadArgs in;
+  const float *row_stats, *entropy, *grad_logp, *grad_entropy;
+  void* grad_hidden;  // bf16 [rows][hidden]
+  void* grad_head;    // bf16 [vocab][hidden]
+};
+size_t head_grad_workspace(int rows, int vocab, int hidden);
+void launch_head_logprobs_grad(const HeadGrad& a, void* workspace, hipStream_t s);

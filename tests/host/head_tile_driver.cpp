@@ -1,0 +1,161 @@
+// CPU-only check of csrc/head_tile.h: every load and store that the products of the lm_head operators make, for tiles at the
+// corners of many sizes, stays inside its array; every tile is visited once; and what fragments read from LDS is what
+// they should hold.  Built and run by tests/test_host_head_tile.py.
+#include <cstdio>
+#include <cstdlib>
+#include <set>
+#include <vector>
+
+#include "../../paper_2506_06122_amd/csrc/head_tile.h"
+
+static long long checks = 0;
+[[noreturn]] static void bad(const char* what, const char* product, long long a, long long b, long long c, long long d) {
+  std::fprintf(stderr, "%s: %s (%lld, %lld, %lld, %lld)\n", product, what, a, b, c, d);
+  std::exit(1);
+}
+
+struct Array {
+  long long bytes;
+};
+struct Product {
+  const char* name;
+  bool pad_rows;
+  Array a, b, out;
+  long long a_pitch, b_pitch, out_pitch, out_size;
+  int M, N, K, capacity, splits;
+  int count;       // what the device finds, -1: nothing
+  bool count_is_k;
+  long long plane_rows;
+};
+
+template <int C, bool KM>
+static void loads(const char* name, long long base, int limit, int k_left, long long pitch, const Array& arr) {
+  using S = HeadSlice<C, KM>;
+  for (int u = 0; u < S::units; ++u)
+    for (int lane = 0; lane < 64; ++lane) {
+      const long long off = S::source(u, lane, limit, k_left, pitch), at = base + off;
+      if (off < 0 || off >= 1ll << 32) bad("offset does not fit", name, u, lane, limit, off);
+      if (at < 0 || at + 16 > arr.bytes) bad("load out of range", name, u, lane, at, arr.bytes);
+      if (at % 16) bad("load not aligned", name, u, lane, at, 0);
+      ++checks;
+    }
+}
+
+template <int BM, int BN, bool AK, bool BK>
+static void walk(const Product& p) {
+  const int m_tiles = head_ceil(p.pad_rows ? p.capacity : p.M, BM), n_tiles = head_ceil(p.N, BN), per = head_ceil(head_ceil(p.K, 32), p.splits);
+  const int tiles = m_tiles * n_tiles * p.splits, M = p.count >= 0 && !p.count_is_k ? p.count : p.M, K = p.count >= 0 && p.count_is_k ? p.count : p.K;
+  if (tiles < 20000) {
+    std::vector<char> seen(tiles, 0);
+    for (int i = 0; i < head_blocks(tiles); ++i) {
+      const HeadBlock b = head_block(i, m_tiles, n_tiles, p.splits);
+      if (!b.inside) continue;
+      if (b.m < 0 || b.m >= m_tiles || b.n >= n_tiles || b.z >= p.splits || seen[(b.z * n_tiles + b.n) * m_tiles + b.m]++) bad("tile twice", p.name, i, b.m, b.n, b.z);
+    }
+    for (char c : seen)
+      if (!c) bad("tile missing", p.name, tiles, 0, 0, 0);
+  }
+  std::set<int> ms{0, m_tiles / 2, m_tiles - 1, head_max(0, m_tiles - 2)}, ns{0, n_tiles - 1}, zs{0, p.splits / 2, p.splits - 1};
+  for (int i = 0; i < m_tiles; ++i)  // tiles around the end of the rows that the device finds
+    if (M / BM >= i - 1 && M / BM <= i + 1) ms.insert(i);
+  for (int m : ms)
+    for (int n : ns)
+      for (int z : zs) {
+        const int m0 = m * BM, n0 = n * BN;
+        const HeadExtent x = head_extent(AK, BK, p.pad_rows, m0, n0, z, M, p.N, K, per, p.a_pitch, p.capacity);
+        if (m0 >= x.m_end) continue;
+        std::set<int> kts;
+        if (x.kt_begin < x.kt_end) kts = {x.kt_begin, x.kt_end - 1, (x.kt_begin + x.kt_end) / 2};
+        for (int kt : kts) {
+          const long long a0 = 2 * (AK ? m0 + kt * 32 * p.a_pitch : m0 * p.a_pitch + kt * 32), b0 = 2 * (BK ? n0 + kt * 32 * p.b_pitch : n0 * p.b_pitch + kt * 32);
+          loads<BM, AK>(p.name, a0, x.a_limit, 32, p.a_pitch, p.a);
+          loads<BN, BK>(p.name, b0, x.b_limit, BK && kt == x.k_tiles - 1 ? x.b_last : 32, p.b_pitch, p.b);
+        }
+        // stores of four values: last row of the tile, last column that passes the kernel's test
+        const int row = head_min(m0 + BM, x.m_end) - 1;
+        const int cols = p.pad_rows ? (int)p.out_pitch : p.N, col = head_min(n0 + BN, cols) - 4;
+        const long long at = ((z * p.plane_rows + row) * p.out_pitch + col) * p.out_size;
+        if (p.out.bytes && (at < 0 || at + 4 * p.out_size > p.out.bytes)) bad("store out of range", p.name, row, col, at, p.out.bytes);
+        ++checks;
+      }
+}
+template <bool AK, bool BK>
+static void by_tile(const Product& p) {
+  const HeadTile t = head_tile(p.M, p.N);
+  if (t.m == 16 && t.n == 256) walk<16, 256, AK, BK>(p);
+  else if (t.m == 32 && t.n == 256) walk<32, 256, AK, BK>(p);
+  else if (t.m == 64 && t.n == 256) walk<64, 256, AK, BK>(p);
+  else if (t.m == 128 && t.n == 128) walk<128, 128, AK, BK>(p);
+  else if (t.m == 256 && t.n == 256) walk<256, 256, AK, BK>(p);
+  else bad("unknown tile", p.name, t.m, t.n, 0, 0);
+}
+
+static void sizes(int rows, int vocab, int hidden, int pad) {
+  const long long hp = hidden + pad;
+  const Array states{(rows - 1) * hp * 2 + hidden * 2}, head{(vocab - 1) * hp * 2 + hidden * 2ll};
+  const HeadTile t = head_tile(rows, vocab);
+  by_tile<false, false>({"logits", false, states, head, {0}, hp, hp, 0, 0, rows, vocab, hidden, 0, 1, -1, false, 0});
+  if (head_ceil(vocab, t.n) < 1) bad("no parts", "logits", vocab, t.n, 0, 0);
+  const HeadGradPlan g = head_grad_plan(rows, vocab, hidden);
+  const Array h{(long long)g.rows * hidden * 2}, dx{(long long)g.rows * g.chunk * 2}, planes{(long long)g.splits * rows * hidden * 4};
+  for (int count : {0, 1, rows / 3, rows / 2 + 1, rows - 1, rows}) {
+    if (count < 0 || count > rows) continue;
+    for (int v0 = 0; v0 < vocab; v0 += g.chunk) {
+      const int v = head_min(g.chunk, vocab - v0), pitch = head_grad_pitch(v);
+      if (pitch > g.chunk || pitch % 256 || pitch < v) bad("pitch", "gradients", pitch, g.chunk, v, 0);
+      const Array w{(long long)(v - 1) * hp * 2 + hidden * 2ll + (long long)(vocab - v0 - v) * hp * 2};
+      by_tile<false, false>({"gradients", true, h, w, dx, hidden, hp, pitch, 2, rows, v, hidden, g.rows, 1, count, false, 0});
+      by_tile<false, true>({"grad_hidden", false, dx, w, planes, pitch, hp, hidden, 4, rows, hidden, v, 0, head_min(g.splits, head_ceil(v, 32)), count, false, rows});
+      by_tile<true, true>({"grad_head", false, dx, h, {(long long)v * hidden * 2}, pitch, hidden, hidden, 2, v, hidden, g.rows, 0, 1, count, true, 0});
+    }
+  }
+}
+
+// LDS after the loads of a slice, then what fragments read from it: value (row, step) as row * 32 + step
+template <int C, bool KM>
+static void fragments() {
+  using S = HeadSlice<C, KM>;
+  const long long pitch = KM ? 1000 * 8 : 64;  // any
+  std::vector<int> lds(C * 32, -1);
+  for (int u = 0; u < S::units; ++u)
+    for (int lane = 0; lane < 64; ++lane) {
+      const long long v = S::source(u, lane, C, 32, pitch) / 2;
+      for (int e = 0; e < 8; ++e) {
+        const int row = KM ? (int)(v % pitch) + e : (int)(v / pitch), k = KM ? (int)(v / pitch) : (int)(v % pitch) + e;
+        lds[(u * 1024 + lane * 16) / 2 + e] = row * 32 + k;
+      }
+    }
+  for (int i = 0; i < C / 16; ++i)
+    for (int lane = 0; lane < 64; ++lane) {
+      const int r = lane & 15, g = lane >> 4;
+      for (int e = 0; e < 8; ++e) {
+        int got;
+        if (KM) {  // element e of lane r: value r % 4 of what lane 4 (e % 4) + r / 4 of the group points at, the second half four steps on
+          const int from = S::fragment(i, g * 16 + 4 * (e & 3) + (r >> 2)) + (e >> 2) * 4 * S::pitch;
+          got = lds[from / 2 + (r & 3)];
+        } else {
+          got = lds[S::fragment(i, lane) / 2 + e];
+        }
+        if (got != (16 * i + r) * 32 + 8 * g + e) bad("fragment", KM ? "K outermost" : "rows outermost", C, i, lane, e);
+        ++checks;
+      }
+    }
+}
+
+int main() {
+  fragments<16, false>();
+  fragments<32, false>();
+  fragments<64, false>();
+  fragments<128, false>();
+  fragments<256, false>();
+  fragments<16, true>();
+  fragments<32, true>();
+  fragments<64, true>();
+  fragments<128, true>();
+  fragments<256, true>();
+  for (int rows : {1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 613, 1500, 4096, 70001})
+    for (int vocab : {1, 2, 31, 32, 33, 100, 255, 256, 257, 300, 513, 1024, 4099, 32001, 151936, 152064})
+      for (int hidden : {32, 64, 96, 128, 160, 256, 288, 1536, 3584})
+        sizes(rows, vocab, hidden, hidden % 64 ? 8 : 0);
+  std::printf("%lld checks\n", checks);
+}

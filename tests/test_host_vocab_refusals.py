@@ -29,6 +29,12 @@ EMBED = dict(table=ARRAY, dtype=1, vocab=100, hidden=64, table_stride=64, tokens
 EMBED_GRAD = dict(grad_rows=ARRAY, dtype=1, n=3, vocab=100, hidden=64, row_stride=64, tokens=ARRAY, scale=1.0, base=None,
                   table_dtype=1, workspace=ARRAY, workspace_bytes=1 << 20, stream=None, grad_table=ARRAY)
 
+HEAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stride=64, rows=3, vocab=100, hidden=64, temperature=1.0,
+            targets=ARRAY, workspace=ARRAY, workspace_bytes=1 << 20, stream=None, logp=ARRAY, entropy=ARRAY, row_stats=ARRAY)
+HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stride=64, rows=3, vocab=100, hidden=64,
+                 temperature=1.0, targets=ARRAY, row_stats=ARRAY, entropy=ARRAY, grad_logp=ARRAY, grad_entropy=ARRAY,
+                 workspace=ARRAY, workspace_bytes=1 << 20, stream=None, grad_hidden=ARRAY, grad_head=ARRAY)
+
 
 @pytest.mark.parametrize("name,args,changed,word", [
     ("rollout_token_logprobs", TOKENS, dict(logits=None), "logits"),
@@ -80,6 +86,35 @@ EMBED_GRAD = dict(grad_rows=ARRAY, dtype=1, n=3, vocab=100, hidden=64, row_strid
     ("rollout_embed_grad", EMBED_GRAD, dict(workspace_bytes=16), "workspace"),
     ("rollout_embed_grad", EMBED_GRAD, dict(workspace=None), "workspace"),
     ("rollout_embed_grad", EMBED_GRAD, dict(base=ARRAY + 1), "base"),
+    ("rollout_head_logprobs", HEAD, dict(hidden_states=None), "hidden_states"),
+    ("rollout_head_logprobs", HEAD, dict(hidden_states=ARRAY + 8), "aligned"),
+    ("rollout_head_logprobs", HEAD, dict(lm_head=None), "lm_head"),
+    ("rollout_head_logprobs", HEAD, dict(lm_head=ARRAY + 2), "aligned"),
+    ("rollout_head_logprobs", HEAD, dict(hidden=48, hidden_stride=48, head_stride=48), "multiple of 32"),
+    ("rollout_head_logprobs", HEAD, dict(hidden_stride=68), "hidden_stride"),
+    ("rollout_head_logprobs", HEAD, dict(hidden_stride=56), "hidden_stride"),
+    ("rollout_head_logprobs", HEAD, dict(head_stride=(1 << 22) + 8), "head_stride"),
+    ("rollout_head_logprobs", HEAD, dict(workspace_bytes=64), "workspace"),
+    ("rollout_head_logprobs", HEAD, dict(workspace=ARRAY + 4), "aligned"),
+    ("rollout_head_logprobs", HEAD, dict(temperature=0.0), "temperature"),
+    ("rollout_head_logprobs", HEAD, dict(vocab=0), "vocab"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden_states=None), "hidden_states"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden_states=ARRAY + 8), "aligned"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(lm_head=None), "lm_head"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(lm_head=ARRAY + 2), "aligned"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden=48, hidden_stride=48, head_stride=48), "multiple of 32"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden_stride=68), "hidden_stride"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden_stride=56), "hidden_stride"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(head_stride=(1 << 22) + 8), "head_stride"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(workspace_bytes=64), "workspace"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(workspace=ARRAY + 4), "aligned"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(temperature=0.0), "temperature"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(vocab=0), "vocab"),
+    ("rollout_head_logprobs", HEAD, dict(logp=None), "logp"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_hidden=None), "grad_hidden"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_head=ARRAY + 8), "aligned"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(entropy=None), "entropy"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_logp=None), "grad_logp"),
 ])
 def test_refused(name, args, changed, word):
     rc, text = call(name, args, **changed)
@@ -90,6 +125,7 @@ def test_nothing_to_do_is_done():
     assert call("rollout_token_logprobs", TOKENS, rows=0, logits=None, logp=None)[0] == 0
     assert call("rollout_token_logprobs_grad", GRAD, rows=0, logits=None)[0] == 0
     assert call("rollout_embed", EMBED, n=0, out=None)[0] == 0
+    assert call("rollout_head_logprobs", HEAD, rows=0, hidden_states=None)[0] == 0
 
 
 def test_workspace_sizes():
@@ -106,7 +142,8 @@ def test_workspace_sizes():
 def test_the_binding_takes_gpu_tensors(bad):
     x, t = torch.zeros(2, 8), torch.zeros(2, dtype=torch.int32)
     for f in (lambda: R.rollout_token_logprobs(x, t), lambda: R.rollout_token_logprobs_grad(x, t, x[:, :2], x[:, 0], x[:, 0]),
-              lambda: R.rollout_embed(x, t), lambda: R.rollout_embed_grad(x, t, 4)):
+              lambda: R.rollout_embed(x, t), lambda: R.rollout_embed_grad(x, t, 4),
+              lambda: R.rollout_head_logprobs(x, x, t), lambda: R.rollout_head_logprobs_grad(x, x, t, x[:, :2], x[:, 0], x[:, 0])):
         with pytest.raises(R.RolloutError) as e:
             f()
         assert e.value.code == B.E_INVAL
