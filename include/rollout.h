@@ -410,7 +410,7 @@ int rollout_embed_grad(const void *grad_rows, int32_t dtype, int32_t n, int32_t 
                        size_t workspace_bytes, void *hip_stream, void *grad_table);
 
 /* rollout_token_logprobs of the logits x = hidden_states . lm_head^T, which never reach memory: bf16 hidden_states
- * [rows][hidden] and lm_head [vocab][hidden], products summed in fp32.  hidden a multiple of 32, rows of both arrays
+ * [rows][hidden] and lm_head [vocab][hidden], products summed in fp32.  hidden a multiple of 64, rows of both arrays
  * aligned to 16 bytes. */
 int64_t rollout_head_logprobs_workspace(int32_t rows, int32_t vocab, int32_t hidden);
 int rollout_head_logprobs(const void *hidden_states, int64_t hidden_stride, const void *lm_head, int64_t head_stride,

@@ -678,7 +678,7 @@ def _head(hidden_states, lm_head, targets):
 
 def rollout_head_logprobs(hidden_states, lm_head, targets=None, *, temperature=1.0, stream=None):
     """rollout_token_logprobs of the logits hidden_states . lm_head^T without storing them: bfloat16 CUDA tensors
-    [rows][hidden] and [vocab][hidden], hidden a multiple of 32.  Returns (logp, entropy, row_stats).  Stream as in
+    [rows][hidden] and [vocab][hidden], hidden a multiple of 64.  Returns (logp, entropy, row_stats).  Stream as in
     rollout_token_logprobs."""
     import torch
     lib = load_library()

@@ -80,7 +80,7 @@ void check_gradients(const float* row_stats, const float* entropy, const float* 
 HeadArgs head_args(const void* hidden_states, int64_t hidden_stride, const void* lm_head, int64_t head_stride, int rows,
                    int vocab, int hidden, float temperature, const int32_t* targets) {
   check_sizes(rows, vocab, hidden);
-  if (hidden % 32) fail(ROLLOUT_E_INVAL, "hidden must be a multiple of 32");
+  if (hidden % 64) fail(ROLLOUT_E_INVAL, "hidden must be a multiple of 64");
   check_operand_stride(hidden_stride, hidden, "hidden_stride");
   check_operand_stride(head_stride, hidden, "head_stride");
   check_optional(targets, 4, "targets");

@@ -8,14 +8,16 @@ constexpr int head_max(int a, int b) { return a > b ? a : b; }
 constexpr int head_ceil(long long a, long long b) { return (int)((a + b - 1) / b); }
 constexpr int head_up(int v, int to) { return (v + to - 1) / to * to; }
 
-// The 32-deep slice of an operand of C columns (rows of C's other side): 64 C bytes of LDS, C / 16 loads of 1 KiB.
-//   rows outermost (KM = false): row by row 64 bytes; the 16-byte chunk c of row r lies in slot c ^ (r / 4 % 4), so that the
-//     16 rows a fragment read touches at a time fill all banks
+constexpr int kHeadDeep = 64;  // steps of K in a stage: with rows outermost a whole line of each row
+
+// The 64-deep slice of an operand of C columns (rows of C's other side): 128 C bytes of LDS, C / 8 loads of 1 KiB.
+//   rows outermost (KM = false): row by row 128 bytes; the 16-byte chunk c of row r lies in slot c ^ (r % 8), so that the
+//     8 rows a fragment read touches at a time fill all banks
 //   K outermost (KM = true): step by step 2 C bytes; chunk c of step k lies in slot c ^ 2 (k % 4 + 4 (k / 8 % 2)), which
 //     spreads the eight steps that half a wavefront reads
 template <int C, bool KM>
 struct HeadSlice {
-  static constexpr int units = C / 16, pitch = 2 * C, chunks = C / 8;
+  static constexpr int units = C / 8, pitch = 2 * C, chunks = C / 8;
   static constexpr int swizzle(int k) { return 2 * ((k & 3) + 4 * (k >> 3 & 1)) & (chunks - 1); }
   // byte offset in memory, from the slice's first value, of lane's 16 bytes of unit u; rows (columns) past `limit` and
   // steps past k_left read the last one
@@ -24,32 +26,58 @@ struct HeadSlice {
       const int at = u * 1024 + lane * 16, k = at / pitch, slot = at % pitch / 16, col = (slot ^ swizzle(k)) * 8;
       return (head_min(k, k_left - 1) * op_pitch + head_min(col, limit - 8)) * 2;
     }
-    const int row = u * 16 + (lane >> 2), chunk = (lane & 3) ^ (lane >> 4);
+    const int row = u * 8 + (lane >> 3), chunk = (lane & 7) ^ (row & 7);
     return (head_min(row, limit - 1) * op_pitch + chunk * 8) * 2;
   }
-  // LDS byte of a lane's part of the fragment of columns 16 i ..: lane = 16 g + r.  Rows outermost: the 16 bytes of
-  // column r, steps 8 g ...  K outermost: 8 bytes of step 8 g + r / 4, columns 4 (r % 4) ..., and again four steps on;
-  // the transposing read exchanges them among the 16 lanes of g, so that lane r gets column r of the four steps.
-  static constexpr int fragment(int i, int lane) {
+  // LDS byte of a lane's part of the fragment of columns 16 i .., steps 32 half ..: lane = 16 g + r.  Rows outermost: the
+  // 16 bytes of column r, steps 8 g ...  K outermost: 8 bytes of step 8 g + r / 4, columns 4 (r % 4) ..., and again four
+  // steps on; the transposing read exchanges them among the 16 lanes of g, so that lane r gets column r of the four steps.
+  static constexpr int fragment(int i, int half, int lane) {
     const int r = lane & 15, g = lane >> 4;
     if (KM) {
       const int k = 8 * g + (r >> 2), chunk = (2 * i + (r >> 1 & 1)) ^ swizzle(k);
-      return k * pitch + chunk * 16 + (r & 1) * 8;
+      return (32 * half + k) * pitch + chunk * 16 + (r & 1) * 8;
     }
-    return i * 1024 + r * 64 + (g ^ (r >> 2)) * 16;
+    return i * 2048 + r * 128 + ((4 * half + g) ^ (r & 7)) * 16;
   }
 };
 
-// Workgroup -> tile.  Consecutive workgroups go to the eight XCDs in turn: each XCD takes a contiguous share of the tiles,
-// all row blocks of a column block before the next, so that a column block's slices are fetched into one L2.
+// Workgroup -> tile.  Consecutive workgroups go to the eight XCDs in turn, each with an L2 of its own, so tiles go to an XCD in
+// groups of group_m x group_n that run side by side there and share their operands' slices; groups go round the XCDs, down
+// the rows first.
+struct HeadGrid {
+  int m_tiles, n_tiles, splits;
+  int group_m, group_n, m_groups, n_groups;
+};
 struct HeadBlock {
   int m, n, z;
   bool inside;
 };
-constexpr int head_blocks(int tiles) { return 8 * head_ceil(tiles, 8); }
-constexpr HeadBlock head_block(unsigned index, int m_tiles, int n_tiles, int splits) {
-  const int tiles = m_tiles * n_tiles * splits, per = (tiles + 7) / 8, t = (int)(index & 7) * per + (int)(index >> 3);
-  return HeadBlock{t % m_tiles, t / m_tiles % n_tiles, t / (m_tiles * n_tiles), t < tiles};
+constexpr HeadGrid head_grid(int m_tiles, int n_tiles, int splits) {
+  // 32 tiles side by side, one to a CU, about as many rows as columns; smaller groups where the XCDs would get too few
+  HeadGrid g{m_tiles, n_tiles, splits, head_min(8, m_tiles), 0, 0, 0};
+  g.group_n = head_min(32 / g.group_m, n_tiles);
+  for (;;) {
+    g.m_groups = head_ceil(m_tiles, g.group_m);
+    g.n_groups = head_ceil(n_tiles, g.group_n);
+    if (g.m_groups * g.n_groups * splits >= 64 || (g.group_m == 1 && g.group_n == 1)) return g;
+    (g.group_n >= g.group_m ? g.group_n : g.group_m) = (head_max(g.group_n, g.group_m) + 1) / 2;
+  }
+}
+// the same for the first rows of it alone: never more workgroups
+constexpr HeadGrid head_grid_rows(HeadGrid g, int m_tiles) {
+  g.m_tiles = m_tiles;
+  g.m_groups = head_max(1, head_ceil(m_tiles, g.group_m));
+  g.group_m = head_max(1, head_ceil(m_tiles, g.m_groups));
+  return g;
+}
+constexpr int head_blocks(const HeadGrid& g) { return head_up(g.m_groups * g.n_groups * g.splits, 8) * g.group_m * g.group_n; }
+constexpr HeadBlock head_block(unsigned index, const HeadGrid& g) {
+  const int per = g.group_m * g.group_n, idx = (int)(index >> 3), in = idx % per;
+  const int group = idx / per * 8 + (int)(index & 7), across = group / g.m_groups;
+  const int m = group % g.m_groups * g.group_m + in % g.group_m, n = across % g.n_groups * g.group_n + in / g.group_m;
+  const int z = across / g.n_groups;
+  return HeadBlock{m, n, z, m < g.m_tiles && n < g.n_tiles && z < g.splits};
 }
 
 // Rows and columns of the tiles that an M x N product is cut into
@@ -71,7 +99,7 @@ struct HeadGradPlan {
 };
 constexpr HeadGradPlan head_grad_plan(int rows, int vocab, int hidden) {
   HeadGradPlan g{};
-  g.rows = head_up(head_max(rows, 1), 32);
+  g.rows = head_up(head_max(rows, 1), kHeadDeep);
   // up to 4 GiB of gradients of logits at a time
   const long long fit = ((long long)4 << 30) / (2ll * g.rows) / 256 * 256, all = head_up(vocab, 256);
   g.chunk = (int)(fit < 256 ? 256 : fit < all ? fit : all);
@@ -93,14 +121,14 @@ struct HeadExtent {
 constexpr HeadExtent head_extent(bool a_km, bool b_km, bool pad_rows, int m0, int n0, int z, int M, int N, int K, int per_split,
                                  long long a_pitch, int row_capacity) {
   HeadExtent x{};
-  x.m_end = pad_rows ? head_min(row_capacity, head_up(M, 32)) : M;
-  x.k_tiles = (K + 31) >> 5;
+  x.m_end = pad_rows ? head_min(row_capacity, head_up(M, kHeadDeep)) : M;
+  x.k_tiles = head_ceil(K, kHeadDeep);
   x.kt_begin = z * per_split;
   x.kt_end = head_min(x.k_tiles, x.kt_begin + per_split);
   // (with K outermost a row of A ends at its pitch, past the last column that is stored; with rows outermost the padding
   // rows exist too, as zeros)
   x.a_limit = (a_km ? (int)a_pitch : x.m_end) - m0;
   x.b_limit = N - n0;
-  x.b_last = b_km ? K - (x.k_tiles - 1) * 32 : 32;
+  x.b_last = b_km ? K - (x.k_tiles - 1) * kHeadDeep : kHeadDeep;
   return x;
 }

@@ -38,14 +38,14 @@ struct Product {
   const int* count;     // device: where not NULL, M (or K, with `count_is_k`) is *count
   bool count_is_k;
   int splits, k_tiles_per_split;
-  int m_tiles, n_tiles; // of the grid
+  HeadGrid grid;
   void* out;
   long long out_pitch;
   bool add;
   float inv_temp;
   // TO_SUMS
   const int* targets;
-  RowSums* sums;        // [M][n_tiles]
+  RowSums* sums;        // [M][grid.n_tiles]
   float* target_logit;  // [M]
   // TO_GRAD: rows of A are rows active[.] of the caller's arrays; columns start at col0 of the vocabulary
   const int* active;
@@ -67,10 +67,10 @@ __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>
   (f(std::integral_constant<int, I>{}), ...);
 }
 
-// Fragment i of a slice in LDS
+// Fragment i of half a slice in LDS
 template <int C, bool KM>
-__device__ __forceinline__ u32x4 fragment(const char* slice, int i, int lane) {
-  const char* p = slice + HeadSlice<C, KM>::fragment(i, lane);
+__device__ __forceinline__ u32x4 fragment(const char* slice, int i, int half, int lane) {
+  const char* p = slice + HeadSlice<C, KM>::fragment(i, half, lane);
   if constexpr (KM) {
     typedef __attribute__((address_space(3))) s16x4* lds_t;
     struct Two {
@@ -85,11 +85,11 @@ __device__ __forceinline__ u32x4 fragment(const char* slice, int i, int lane) {
 }
 
 // A workgroup computes BM = 16 WM MT rows x BN = 16 WN NT columns of C; its WM x WN wavefronts own MT x NT tiles of 16 x 16
-// each.  Slices of 32 steps of K go straight from memory into a ring of S LDS stages; the fragments of stage s + 1 are read,
-// and the copies of stage s + S issued, between the products of stage s, with one barrier per stage: it says that every
-// wavefront's copies of stage s + 1 have arrived (loads are counted in order, later stages stay in flight) and that
-// everyone holds stage s in registers.  The copies past the end of K repeat the last slice, so that every stage counts
-// the same number of them.
+// each.  Slices of 64 steps of K go straight from memory into a ring of S LDS stages.  A stage is multiplied in two halves:
+// while the first is, the second's fragments are read; then one barrier says that every wavefront holds the whole stage
+// in registers, so that its buffer takes the copies of stage s + S, and that stage s + 1 has arrived (loads are counted
+// in order, later stages stay in flight), whose first half is read while the second is multiplied.  The copies past the
+// end of K repeat the last slice, so that every stage counts the same number of them.
 template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
 __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_product_kernel(Product p) {
   constexpr bool WIDE = MT * NT >= 32;
@@ -97,14 +97,18 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
   using A = HeadSlice<BM, AK>;
   using B = HeadSlice<BN, BK>;
   constexpr int U = A::units + B::units, L = (U + NW - 1) / NW, STAGE = U * 1024;
-  static_assert(S * STAGE <= 160 * 1024 && S >= 2 && (S - 1) * L < 64, "fits the CU and the load counter");
-  __shared__ __attribute__((aligned(1024))) char lds[S * STAGE];
+  // results on their way out: a wavefront's rows of bf16, 16 bytes past its width so that rows do not share banks
+  constexpr int OUT_ROW = NT * 32 + 16, OUT_WAVE = MT * 16 * OUT_ROW, OUT = TO == TO_BF16 || TO == TO_GRAD ? NW * OUT_WAVE : 0;
+  constexpr int EXTRA = TO == TO_GRAD ? BM * (int)sizeof(RowGrad) : TO == TO_SUMS ? WN * BM * (int)sizeof(RowSums) : 0;
+  constexpr int LDS = S * STAGE > OUT + EXTRA ? S * STAGE : OUT + EXTRA;
+  static_assert(LDS <= 160 * 1024 && S >= 2 && (S - 1) * L < 64, "fits the CU and the load counter");
+  __shared__ __attribute__((aligned(1024))) char lds[LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const HeadBlock block = head_block(blockIdx.x, p.m_tiles, p.n_tiles, p.splits);
+  const int M = p.count && !p.count_is_k ? *p.count : p.M, K = p.count && p.count_is_k ? *p.count : p.K;
+  const HeadBlock block = head_block(blockIdx.x, head_grid_rows(p.grid, head_ceil(TO == TO_GRAD ? head_up(M, kHeadDeep) : M, BM)));
   if (!block.inside) return;
   const int bn = block.n, bz = block.z;
-  const int M = p.count && !p.count_is_k ? *p.count : p.M, K = p.count && p.count_is_k ? *p.count : p.K;
   const int m0 = block.m * BM, n0 = bn * BN;
   const HeadExtent x = head_extent(AK, BK, TO == TO_GRAD, m0, n0, bz, M, p.N, K, p.k_tiles_per_split, p.a.pitch, p.row_capacity);
   if (m0 >= x.m_end) return;
@@ -120,7 +124,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
     // this wavefront's loads of a stage: units wave, wave + NW, ... of A's, then B's; their sources move on with the slices
     unsigned voff[L], tail[L], dst[L];
     bool is_b[L];
-    const long long a_step = AK ? p.a.pitch * 64 : 64, b_step = BK ? p.b.pitch * 64 : 64;
+    const long long a_step = (AK ? p.a.pitch : 1) * 2 * kHeadDeep, b_step = (BK ? p.b.pitch : 1) * 2 * kHeadDeep;
     const char* pa = (const char*)p.a.p + 2 * (AK ? m0 : m0 * p.a.pitch) + kt_begin * a_step;
     const char* pb = (const char*)p.b.p + 2 * (BK ? n0 : n0 * p.b.pitch) + kt_begin * b_step;
 #pragma unroll
@@ -129,14 +133,14 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
       is_b[s] = u >= A::units;
       dst[s] = u * 1024;
       if (!is_b[s]) {
-        tail[s] = voff[s] = (unsigned)A::source(u, lane, x.a_limit, 32, p.a.pitch);
+        tail[s] = voff[s] = (unsigned)A::source(u, lane, x.a_limit, kHeadDeep, p.a.pitch);
       } else {
-        voff[s] = (unsigned)B::source(u - A::units, lane, x.b_limit, 32, p.b.pitch);
+        voff[s] = (unsigned)B::source(u - A::units, lane, x.b_limit, kHeadDeep, p.b.pitch);
         tail[s] = BK ? (unsigned)B::source(u - A::units, lane, x.b_limit, x.b_last, p.b.pitch) : voff[s];
       }
     }
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds;
-    int ahead = kt_begin;  // k-tile of the next copies
+    int ahead = kt_begin;  // slice of the next copies
     auto issue = [&](int s, int buf) __attribute__((always_inline)) {
       const unsigned to = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + dst[s]);
       const unsigned from = BK && ahead == k_tiles - 1 ? tail[s] : voff[s];
@@ -156,18 +160,18 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
       move_on();
     }
     u32x4 a[2][MT], b[2][NT];
-    constexpr int NR = MT + NT, NM = MT * NT, NS = NR + L;
-    auto read = [&](int y, const char* st, int f) __attribute__((always_inline)) {  // in the order in which they are multiplied
-      if (f < 1) a[y][0] = fragment<BM, AK>(st, wm * MT, lane);
-      else if (f < 1 + NT) b[y][f - 1] = fragment<BN, BK>(st + A::units * 1024, wn * NT + f - 1, lane);
-      else a[y][f - NT] = fragment<BM, AK>(st, wm * MT + f - NT, lane);
+    constexpr int NR = MT + NT, NM = MT * NT;
+    auto read = [&](int half, const char* st, int f) __attribute__((always_inline)) {  // in the order in which they are multiplied
+      if (f < 1) a[half][0] = fragment<BM, AK>(st, wm * MT, half, lane);
+      else if (f < 1 + NT) b[half][f - 1] = fragment<BN, BK>(st + A::units * 1024, wn * NT + f - 1, half, lane);
+      else a[half][f - NT] = fragment<BM, AK>(st, wm * MT + f - NT, half, lane);
     };
-    auto mul = [&](int y, int q) __attribute__((always_inline)) {
+    auto mul = [&](int half, int q) __attribute__((always_inline)) {
       const int i = q / NT, j = q % NT;
-      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[y][j]),
-                                                          __builtin_bit_cast(bf16x8, a[y][i]), acc[i][j], 0, 0, 0);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, b[half][j]),
+                                                          __builtin_bit_cast(bf16x8, a[half][i]), acc[i][j], 0, 0, 0);
     };
-    auto keep_sums = [&]() __attribute__((always_inline)) {  // in the accumulation registers at the end of each stage
+    auto keep_sums = [&]() __attribute__((always_inline)) {  // in the accumulation registers at the end of each half
       if constexpr (WIDE) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -180,87 +184,69 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
 #pragma unroll
     for (int f = 0; f < NR; ++f) read(0, lds, f);
     int buf = 0;
-    auto stage = [&](int y) __attribute__((always_inline)) {
-      wait_and_barrier<(S - 2) * L>();
-      const int next = buf == S - 1 ? 0 : buf + 1;
-      const char* st = lds + next * STAGE;
+    // products of one half; spread between them, the reads of the other half from st and, with COPIES, a stage's copies
+    auto half_stage = [&](auto halfc, auto copiesc, const char* st) __attribute__((always_inline)) {
+      constexpr int H = decltype(halfc)::value, NS = NR + (decltype(copiesc)::value ? L : 0);
       unrolled([&](auto qc) __attribute__((always_inline)) {
         constexpr int q = decltype(qc)::value, u0 = (q * NS + NM - 1) / NM, u1 = ((q + 1) * NS + NM - 1) / NM;
-        mul(y, q);
+        mul(H, q);
 #pragma unroll
         for (int u = u0; u < u1; ++u) {
-          if (u < NR) read(y ^ 1, st, u);
-          else issue(u - NR, buf);
+          // copies and reads in turn, until either is through
+          constexpr int C = NS - NR, both = 2 * (C < NR ? C : NR);
+          const bool copy = u < both ? u & 1 : C > NR;
+          if (copy) issue(u < both ? u >> 1 : u - NR, buf);
+          else read(H ^ 1, st, u < both ? u >> 1 : u - C);
         }
         __builtin_amdgcn_sched_barrier(0);
       }, std::make_integer_sequence<int, NM>{});
+      keep_sums();
+    };
+    using First = std::integral_constant<int, 0>;
+    using Second = std::integral_constant<int, 1>;
+    for (int left = kt_end - kt_begin; left > 1; --left) {
+      half_stage(First{}, std::false_type{}, lds + buf * STAGE);
+      wait_and_barrier<(S - 2) * L>();
+      const int next = buf == S - 1 ? 0 : buf + 1;
+      half_stage(Second{}, std::true_type{}, lds + next * STAGE);
       move_on();
-      keep_sums();
       buf = next;
-    };
-    auto last = [&](int y) __attribute__((always_inline)) {
-      unrolled([&](auto qc) __attribute__((always_inline)) { mul(y, decltype(qc)::value); }, std::make_integer_sequence<int, NM>{});
-      keep_sums();
-    };
-    int left = kt_end - kt_begin;
-    for (; left > 2; left -= 2) {
-      stage(0);
-      stage(1);
     }
-    if (left == 2) {
-      stage(0);
-      last(1);
-    } else {
-      last(0);
-    }
+    half_stage(First{}, std::false_type{}, lds + buf * STAGE);
+    unrolled([&](auto qc) __attribute__((always_inline)) { mul(1, decltype(qc)::value); }, std::make_integer_sequence<int, NM>{});
+    keep_sums();
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may still be on its way into LDS
   }
+  __syncthreads();
   // acc[i][j][e]: row 16 (wm MT + i) + r, column 16 (wn NT + j) + 4 g + e of the tile
-  const int col = n0 + wn * NT * 16 + 4 * g;
+  const int col0 = n0 + wn * NT * 16, col = col0 + 4 * g;
+  const bool whole = n0 + BN <= p.N;
 
   if constexpr (TO == TO_SUMS) {
     const float c = p.inv_temp * kLog2e;
-    __syncthreads();
     RowSums* part = (RowSums*)lds;  // [WN][BM]
-    const bool whole = n0 + BN <= p.N;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int ml = (wm * MT + i) * 16 + r, m = m0 + ml;
-      // the target's place among this lane's values, if it is one of them: 4 j + e
-      const int target = p.targets && m < M ? p.targets[m] : -1;
-      const int from = target - (n0 + wn * NT * 16), place = (from >> 4) * 4 + (from & 3);
-      const bool here = target >= 0 && target < p.N && from >= 0 && from < NT * 16 && (from >> 2 & 3) == g;
-      float x_target = 0.f;
-      RowSums s{-3.402823466e38f, 0.f, 0.f};
-      if (!whole) {
+      const int target = p.targets && m < M ? p.targets[m] : -1, from = target - col0;
+      if (__any(target < p.N && from >= 0 && from < NT * 16)) {  // some row's target is among these columns
+        const int place = (from >> 4) * 4 + (from & 3);
+        float x_target = 0.f;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (col + j * 16 + e >= p.N) acc[i][j][e] = -INFINITY;
+          for (int e = 0; e < 4; ++e) x_target = place == 4 * j + e ? acc[i][j][e] : x_target;
+        if (target >= 0 && target < p.N && from >= 0 && from < NT * 16 && (from >> 2 & 3) == g) p.target_logit[m] = x_target;
       }
+      float v[4 * NT];
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x_target = place == 4 * j + e ? acc[i][j][e] : x_target;
-          s.m = fmaxf(s.m, acc[i][j][e]);
-        }
-      if (here) p.target_logit[m] = x_target;
-      s.m = fmaxf(s.m, __shfl_xor(s.m, 16, WAVE));
-      s.m = fmaxf(s.m, __shfl_xor(s.m, 32, WAVE));
+        for (int e = 0; e < 4; ++e) v[4 * j + e] = whole || col + j * 16 + e < p.N ? acc[i][j][e] : -INFINITY;
+      RowSums s{kLowest, 0.f, 0.f};
+      add_chunk<4 * NT>(s, v, c);
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float y = (acc[i][j][e] - s.m) * c, w = __builtin_amdgcn_exp2f(y);
-          s.s += w;
-          s.t = fmaf(w, fmaxf(y, -1e30f), s.t);
-        }
-      s.s += __shfl_xor(s.s, 16, WAVE);
-      s.s += __shfl_xor(s.s, 32, WAVE);
-      s.t += __shfl_xor(s.t, 16, WAVE);
-      s.t += __shfl_xor(s.t, 32, WAVE);
+      for (int o = 16; o < 64; o <<= 1) s = merge(s, RowSums{__shfl_xor(s.m, o, WAVE), __shfl_xor(s.s, o, WAVE), __shfl_xor(s.t, o, WAVE)}, c);
       if (g == 0) part[wn * BM + ml] = s;
     }
     __syncthreads();
@@ -268,67 +254,78 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
       RowSums s = part[ml];
 #pragma unroll
       for (int w = 1; w < WN; ++w) s = merge(s, part[w * BM + ml], c);
-      p.sums[(long long)(m0 + ml) * p.n_tiles + bn] = s;
+      p.sums[(long long)(m0 + ml) * p.grid.n_tiles + bn] = s;
     }
-  } else if constexpr (TO == TO_GRAD) {
-    const float c = p.inv_temp * kLog2e;
-    __syncthreads();
-    RowGrad* rows = (RowGrad*)lds;
-    for (int ml = threadIdx.x; ml < BM; ml += NW * 64) {
-      RowGrad q{};
-      q.none = true;
-      if (m0 + ml < M)
-        q = row_grad(p.row_stats, p.entropy, p.grad_logp, p.grad_entropy, p.targets, p.inv_temp, p.vocab, p.active[m0 + ml]);
-      rows[ml] = q;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int ml = (wm * MT + i) * 16 + r, m = m0 + ml;
-      const RowGrad q = rows[ml];
-      if (m < x.m_end) {
-        const int target = q.target - p.col0;
-        uint16_t* o = (uint16_t*)p.out + m * p.out_pitch;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const int n = col + j * 16;
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[e] = grad_of(acc[i][j][e], c, q);
-            if (n + e == target && q.target >= 0) v[e] += q.at_target;
-            if (q.none || n + e >= p.N) v[e] = 0.f;
-          }
-          if (n < p.out_pitch) {  // columns up to the pitch are the padding of K in the product that follows
-            uint2 w;
-            w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{v[0], v[1]}), bf16_pair));
-            w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{v[2], v[3]}), bf16_pair));
-            *(uint2*)(o + n) = w;
-          }
-        }
-      }
-    }
-  } else {
+  } else if constexpr (TO == TO_PLANE) {
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       const int m = m0 + (wm * MT + i) * 16 + r;
       if (m < M) {
+        f32x4* o = (f32x4*)((float*)p.out + ((long long)bz * p.M + m) * p.out_pitch);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           const int n = col + j * 16;
-          if (n < p.N) {  // N is a multiple of 32
-            if constexpr (TO == TO_PLANE) {
-              f32x4* o = (f32x4*)((float*)p.out + ((long long)bz * p.M + m) * p.out_pitch + n);
-              *o = p.add ? *o + acc[i][j] : acc[i][j];
-            } else {
-              uint2 w;
-              w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][0], acc[i][j][1]}), bf16_pair));
-              w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][2], acc[i][j][3]}), bf16_pair));
-              *(uint2*)((uint16_t*)p.out + m * p.out_pitch + n) = w;
-            }
-          }
+          if (n < p.N) o[n / 4] = p.add ? o[n / 4] + acc[i][j] : acc[i][j];  // N is a multiple of 64
         }
       }
+    }
+  } else {
+    // bf16, through LDS so that rows leave as whole lines
+    char* mine = lds + wave * OUT_WAVE;
+    const RowGrad* rows = (const RowGrad*)(lds + OUT);
+    const float c = p.inv_temp * kLog2e;
+    if constexpr (TO == TO_GRAD) {
+      for (int ml = threadIdx.x; ml < BM; ml += NW * 64) {
+        RowGrad q{};
+        q.none = true;
+        if (m0 + ml < M)
+          q = row_grad(p.row_stats, p.entropy, p.grad_logp, p.grad_entropy, p.targets, p.inv_temp, p.vocab, p.active[m0 + ml]);
+        ((RowGrad*)(lds + OUT))[ml] = q;
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      if constexpr (TO == TO_GRAD) {
+        const RowGrad q = rows[(wm * MT + i) * 16 + r];
+        const int from = q.target - p.col0 - col0, place = (from >> 4) * 4 + (from & 3);
+        const bool here = q.target >= 0 && from >= 0 && from < NT * 16 && (from >> 2 & 3) == g;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = grad_of(acc[i][j][e], c, q);
+        if (__any(here)) {
+          const float add = here ? q.at_target : 0.f;
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] += place == 4 * j + e ? add : 0.f;
+        }
+        if (__any(q.none || !whole)) {
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (q.none || col + j * 16 + e >= p.N) acc[i][j][e] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        uint2 w;
+        w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][0], acc[i][j][1]}), bf16_pair));
+        w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][2], acc[i][j][3]}), bf16_pair));
+        *(uint2*)(mine + (i * 16 + r) * OUT_ROW + j * 32 + g * 8) = w;
+      }
+    }
+    // (only this wavefront's own writes are read: the compiler waits for them)
+    constexpr int LANES = NT * 2, ROWS = 64 / LANES;  // lanes to a row, rows at a time
+    // columns that exist: the product's, or as far as the padding of K in the product that follows
+    const int n = col0 + lane % LANES * 8, n_end = TO == TO_GRAD ? (int)p.out_pitch : p.N;
+#pragma unroll 4
+    for (int q = 0; q < MT * 16; q += ROWS) {
+      const int ml = q + lane / LANES, m = m0 + wm * MT * 16 + ml;
+      const u32x4 w = *(const u32x4*)(mine + ml * OUT_ROW + lane % LANES * 16);
+      if (m < x.m_end && n < n_end) *(u32x4*)((uint16_t*)p.out + m * p.out_pitch + n) = w;
     }
   }
 }
@@ -338,7 +335,7 @@ __global__ __launch_bounds__(256) void head_finish_kernel(HeadArgs in, TokenOut 
   const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (row >= in.rows) return;
   const float c = in.inv_temp * kLog2e;
-  RowSums s{-3.402823466e38f, 0.f, 0.f};
+  RowSums s{kLowest, 0.f, 0.f};
   for (int i = lane; i < parts; i += WAVE) s = merge(s, sums[(long long)row * parts + i], c);
 #pragma unroll
   for (int o = 1; o < WAVE; o <<= 1) s = merge(s, RowSums{__shfl_xor(s.m, o, WAVE), __shfl_xor(s.s, o, WAVE), __shfl_xor(s.t, o, WAVE)}, c);
@@ -378,7 +375,7 @@ __global__ __launch_bounds__(1024) void head_active_kernel(HeadGrad a, int* coun
 // out[i] = hidden_states[active[i]], zeros behind them up to a whole k-tile; one row per workgroup
 __global__ __launch_bounds__(256) void head_gather_kernel(HeadArgs in, const int* count, const int* active, uint16_t* out) {
   const int i = blockIdx.x, n = *count;
-  if (i >= ((n + 31) & ~31)) return;
+  if (i >= head_up(n, kHeadDeep)) return;
   const u32x4* src = i < n ? (const u32x4*)((const uint16_t*)in.hidden_states + active[i] * in.hidden_stride) : nullptr;
   u32x4* dst = (u32x4*)(out + (long long)i * in.hidden);
   const u32x4 zero = {0, 0, 0, 0};
@@ -402,19 +399,18 @@ __global__ __launch_bounds__(256) void head_planes_kernel(const float* planes, i
 // ---- shapes ------------------------------------------------------------------------------------
 template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
 void launch_shape(Product p, hipStream_t s) {
-  p.m_tiles = head_ceil(TO == TO_GRAD ? p.row_capacity : p.M, WM * MT * 16);
-  p.n_tiles = head_ceil(p.N, WN * NT * 16);
-  p.k_tiles_per_split = head_ceil(head_ceil(p.K, 32), p.splits);
-  head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK><<<head_blocks(p.m_tiles * p.n_tiles * p.splits), WM * WN * 64, 0, s>>>(p);
+  p.grid = head_grid(head_ceil(TO == TO_GRAD ? p.row_capacity : p.M, WM * MT * 16), head_ceil(p.N, WN * NT * 16), p.splits);
+  p.k_tiles_per_split = head_ceil(head_ceil(p.K, kHeadDeep), p.splits);
+  head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK><<<head_blocks(p.grid), WM * WN * 64, 0, s>>>(p);
 }
 template <int TO, bool AK, bool BK>
 void launch_product(const Product& p, hipStream_t s) {
   const HeadTile t = head_tile(p.M, p.N);
-  if (t.m == 16) launch_shape<1, 4, 1, 4, 4, TO, AK, BK>(p, s);
-  else if (t.m == 32) launch_shape<1, 4, 2, 4, 4, TO, AK, BK>(p, s);
-  else if (t.m == 64) launch_shape<1, 4, 4, 4, 4, TO, AK, BK>(p, s);
-  else if (t.m == 128) launch_shape<2, 2, 4, 4, 4, TO, AK, BK>(p, s);
-  else launch_shape<2, 2, 8, 8, 4, TO, AK, BK>(p, s);
+  if (t.m == 16) launch_shape<1, 4, 1, 4, 2, TO, AK, BK>(p, s);
+  else if (t.m == 32) launch_shape<1, 4, 2, 4, 2, TO, AK, BK>(p, s);
+  else if (t.m == 64) launch_shape<1, 4, 4, 4, 2, TO, AK, BK>(p, s);
+  else if (t.m == 128) launch_shape<2, 2, 4, 4, 2, TO, AK, BK>(p, s);
+  else launch_shape<2, 2, 8, 8, 2, TO, AK, BK>(p, s);
 }
 
 constexpr size_t piece(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -495,7 +491,7 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
       q.N = in.hidden;
       q.K = v;
       q.count = count;
-      q.splits = std::min(g.splits, std::max(1, ceil_div(v, 32)));
+      q.splits = std::min(g.splits, std::max(1, head_ceil(v, kHeadDeep)));
       q.out = planes;
       q.out_pitch = in.hidden;
       q.add = v0 > 0;

@@ -1,10 +1,10 @@
 // Log-probs of given tokens from logits, with entropy and the most likely alternatives, and the gradient of the logits.
 //
-//   y_v = (x_v - m) log2(e) / T,  S = sum 2^y,  ln p_v = ln2 y_v - ln S,  H = ln S - ln2 (sum y 2^y) / S
+//   y_v = x_v log2(e) / T - r,  S = sum 2^y,  ln p_v = ln2 y_v - ln S,  H = ln S - ln2 (sum y 2^y) / S, for any r
 //
-// One pass over the row: every thread keeps the maximum it has seen, and its two sums relative to that; a chunk of values
-// is taken relative to the new maximum, the old sums are scaled once a chunk.  The pass is bound by memory; the arithmetic
-// (11 issue slots per value, the exponential counting four) comes next.
+// One pass over the row: every thread keeps the maximum it has seen, and its two sums relative to that (RowSums); a chunk of
+// values is taken relative to the new maximum, the old sums are scaled once a chunk.  The pass is bound by memory; the
+// arithmetic (9 issue slots per value, the exponential counting four) comes next.
 //
 // Alternatives ride along for free: the K-th largest of the threads' maxima is a bound that K values reach, and every value
 // that reaches it sits with a thread whose maximum does.  So only those threads' values are read again, spread over the
@@ -64,23 +64,6 @@ struct RowSlice {
   }
   __device__ int values() const { return head_here + (end - begin) * kVec<V> + tail; }
 };
-
-template <int N>
-__device__ inline void add_chunk(RowSums& r, const float* v, float c) {
-  float top = v[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
-  const float m = fmaxf(r.m, top), d = fminf((m - r.m) * c, 1e30f), f = __builtin_amdgcn_exp2f(-d);
-  r.t = (r.t - d * r.s) * f;
-  r.s *= f;
-  r.m = m;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float y = (v[i] - m) * c, e = __builtin_amdgcn_exp2f(y);
-    r.s += e;
-    r.t = fmaf(e, fmaxf(y, -1e30f), r.t);
-  }
-}
 
 __device__ inline RowSums merge_wave(RowSums r, float c) {
 #pragma unroll
@@ -205,7 +188,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOu
   const bool has_target = target >= 0 && target < in.vocab;
   const float x_target = has_target && p.parts == 1 ? to_f32(row.x[target]) : 0.f;
   // the reference starts at the lowest finite value: a row of -inf then has differences of -inf, not NaN
-  RowSums sums{-3.402823466e38f, 0.f, 0.f};
+  RowSums sums{kLowest, 0.f, 0.f};
   float single = -INFINITY;
   const int one = row.single(tid);
   if (one >= 0) single = to_f32(row.x[one]);
@@ -251,7 +234,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOu
     __syncthreads();
     const float log_s = p.parts == 1 ? log_s_s : 0.f;
     // a maximum that is still the start stands for -inf: the bound must not lie above the values themselves
-    const float top = sums.m == -3.402823466e38f ? -INFINITY : sums.m;
+    const float top = sums.m == kLowest ? -INFINITY : sums.m;
     top_of_slice(row, top, has, out.top, sh, [&](int rank, unsigned long long key) {
       if (p.parts == 1) store_top(out, r, rank, key, total.m, log_s, in.inv_temp);
       else p.keys[((long long)r * p.parts + part) * out.top + rank] = key;
@@ -259,8 +242,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOu
   }
 }
 
-// Joins a row's parts.  An alternative of the row is one of its part; keys below the greatest of the parts' last keys
-// cannot be among the first K.
+// Joins a row's parts.  An alternative of the row is one of its part's.
 template <typename V, bool TOP>
 __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut out, TokenParts p) {
   __shared__ RowSums wave_s[NW];
@@ -273,11 +255,8 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
   const int target = in.targets ? in.targets[r] : -1;
   const bool has_target = target >= 0 && target < in.vocab;
   const float x_target = has_target ? to_f32(((const V*)in.logits + r * in.stride)[target]) : 0.f;
-  if (tid == 0) {
-    n_s = 0;
-    least_s = 0;
-  }
-  RowSums mine{-3.402823466e38f, 0.f, 0.f};
+  if (tid == 0) n_s = 0;
+  RowSums mine{kLowest, 0.f, 0.f};
   for (int i = tid; i < p.parts; i += T) mine = merge(mine, p.sums[(long long)r * p.parts + i], c);
   mine = merge_wave(mine, c);
   if (lane == 0) wave_s[wave] = mine;
@@ -287,8 +266,19 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
   for (int w = 1; w < NW; ++w) total = merge(total, wave_s[w], c);
   if (tid == 0) log_s_s = finish_row(total, out, r, has_target, x_target, in.inv_temp);
   if constexpr (TOP) {
+    // Of every part's `deep` greatest keys the last: the `wide`-th greatest of these is a bound that K keys reach
     const unsigned long long* keys = p.keys + (long long)r * p.parts * out.top;
-    for (int i = tid; i < p.parts; i += T) atomicMax(&least_s, keys[(long long)i * out.top + out.top - 1]);
+    const int deep = (out.top + p.parts - 1) / p.parts, wide = (out.top + deep - 1) / deep;
+    if (wave == 0) {
+      const unsigned long long key = lane < p.parts ? keys[(long long)lane * out.top + deep - 1] : 0;
+      int rank = 0;
+      for (int j = 0; j < p.parts; ++j) {
+        const unsigned long long other = (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 |
+                                         (unsigned)__builtin_amdgcn_readlane((int)key, j);
+        rank += other > key || (other == key && j < lane);
+      }
+      if (lane < p.parts && rank == wide - 1) least_s = key;
+    }
     __syncthreads();
     const unsigned long long least = max(least_s, 1ull);
     for (int i = tid; i < p.parts * out.top; i += T) {

@@ -43,12 +43,16 @@ static void loads(const char* name, long long base, int limit, int k_left, long 
 
 template <int BM, int BN, bool AK, bool BK>
 static void walk(const Product& p) {
-  const int m_tiles = head_ceil(p.pad_rows ? p.capacity : p.M, BM), n_tiles = head_ceil(p.N, BN), per = head_ceil(head_ceil(p.K, 32), p.splits);
+  const int m_tiles = head_ceil(p.pad_rows ? p.capacity : p.M, BM), n_tiles = head_ceil(p.N, BN), per = head_ceil(head_ceil(p.K, kHeadDeep), p.splits);
   const int tiles = m_tiles * n_tiles * p.splits, M = p.count >= 0 && !p.count_is_k ? p.count : p.M, K = p.count >= 0 && p.count_is_k ? p.count : p.K;
   if (tiles < 20000) {
     std::vector<char> seen(tiles, 0);
-    for (int i = 0; i < head_blocks(tiles); ++i) {
-      const HeadBlock b = head_block(i, m_tiles, n_tiles, p.splits);
+    const HeadGrid whole = head_grid(m_tiles, n_tiles, p.splits);
+    for (int some = 1; some <= m_tiles; some += 1 + m_tiles / 7)
+      if (head_blocks(head_grid_rows(whole, some)) > head_blocks(whole)) bad("more workgroups", p.name, some, m_tiles, n_tiles, p.splits);
+    const HeadGrid grid = head_grid_rows(whole, m_tiles);
+    for (int i = 0; i < head_blocks(grid); ++i) {
+      const HeadBlock b = head_block(i, grid);
       if (!b.inside) continue;
       if (b.m < 0 || b.m >= m_tiles || b.n >= n_tiles || b.z >= p.splits || seen[(b.z * n_tiles + b.n) * m_tiles + b.m]++) bad("tile twice", p.name, i, b.m, b.n, b.z);
     }
@@ -67,9 +71,9 @@ static void walk(const Product& p) {
         std::set<int> kts;
         if (x.kt_begin < x.kt_end) kts = {x.kt_begin, x.kt_end - 1, (x.kt_begin + x.kt_end) / 2};
         for (int kt : kts) {
-          const long long a0 = 2 * (AK ? m0 + kt * 32 * p.a_pitch : m0 * p.a_pitch + kt * 32), b0 = 2 * (BK ? n0 + kt * 32 * p.b_pitch : n0 * p.b_pitch + kt * 32);
-          loads<BM, AK>(p.name, a0, x.a_limit, 32, p.a_pitch, p.a);
-          loads<BN, BK>(p.name, b0, x.b_limit, BK && kt == x.k_tiles - 1 ? x.b_last : 32, p.b_pitch, p.b);
+          const long long a0 = 2 * (AK ? m0 + kt * kHeadDeep * p.a_pitch : m0 * p.a_pitch + kt * kHeadDeep), b0 = 2 * (BK ? n0 + kt * kHeadDeep * p.b_pitch : n0 * p.b_pitch + kt * kHeadDeep);
+          loads<BM, AK>(p.name, a0, x.a_limit, kHeadDeep, p.a_pitch, p.a);
+          loads<BN, BK>(p.name, b0, x.b_limit, BK && kt == x.k_tiles - 1 ? x.b_last : kHeadDeep, p.b_pitch, p.b);
         }
         // stores of four values: last row of the tile, last column that passes the kernel's test
         const int row = head_min(m0 + BM, x.m_end) - 1;
@@ -105,38 +109,38 @@ static void sizes(int rows, int vocab, int hidden, int pad) {
       if (pitch > g.chunk || pitch % 256 || pitch < v) bad("pitch", "gradients", pitch, g.chunk, v, 0);
       const Array w{(long long)(v - 1) * hp * 2 + hidden * 2ll + (long long)(vocab - v0 - v) * hp * 2};
       by_tile<false, false>({"gradients", true, h, w, dx, hidden, hp, pitch, 2, rows, v, hidden, g.rows, 1, count, false, 0});
-      by_tile<false, true>({"grad_hidden", false, dx, w, planes, pitch, hp, hidden, 4, rows, hidden, v, 0, head_min(g.splits, head_ceil(v, 32)), count, false, rows});
+      by_tile<false, true>({"grad_hidden", false, dx, w, planes, pitch, hp, hidden, 4, rows, hidden, v, 0, head_min(g.splits, head_ceil(v, kHeadDeep)), count, false, rows});
       by_tile<true, true>({"grad_head", false, dx, h, {(long long)v * hidden * 2}, pitch, hidden, hidden, 2, v, hidden, g.rows, 0, 1, count, true, 0});
     }
   }
 }
 
-// LDS after the loads of a slice, then what fragments read from it: value (row, step) as row * 32 + step
+// LDS after the loads of a slice, then what fragments read from it: value (row, step) as row * 64 + step
 template <int C, bool KM>
 static void fragments() {
   using S = HeadSlice<C, KM>;
   const long long pitch = KM ? 1000 * 8 : 64;  // any
-  std::vector<int> lds(C * 32, -1);
+  std::vector<int> lds(C * 64, -1);
   for (int u = 0; u < S::units; ++u)
     for (int lane = 0; lane < 64; ++lane) {
-      const long long v = S::source(u, lane, C, 32, pitch) / 2;
+      const long long v = S::source(u, lane, C, 64, pitch) / 2;
       for (int e = 0; e < 8; ++e) {
         const int row = KM ? (int)(v % pitch) + e : (int)(v / pitch), k = KM ? (int)(v / pitch) : (int)(v % pitch) + e;
-        lds[(u * 1024 + lane * 16) / 2 + e] = row * 32 + k;
+        lds[(u * 1024 + lane * 16) / 2 + e] = row * 64 + k;
       }
     }
-  for (int i = 0; i < C / 16; ++i)
+  for (int i = 0; i < C / 8; ++i)
     for (int lane = 0; lane < 64; ++lane) {
-      const int r = lane & 15, g = lane >> 4;
+      const int half = i & 1, r = lane & 15, g = lane >> 4;
       for (int e = 0; e < 8; ++e) {
         int got;
         if (KM) {  // element e of lane r: value r % 4 of what lane 4 (e % 4) + r / 4 of the group points at, the second half four steps on
-          const int from = S::fragment(i, g * 16 + 4 * (e & 3) + (r >> 2)) + (e >> 2) * 4 * S::pitch;
+          const int from = S::fragment(i >> 1, half, g * 16 + 4 * (e & 3) + (r >> 2)) + (e >> 2) * 4 * S::pitch;
           got = lds[from / 2 + (r & 3)];
         } else {
-          got = lds[S::fragment(i, lane) / 2 + e];
+          got = lds[S::fragment(i >> 1, half, lane) / 2 + e];
         }
-        if (got != (16 * i + r) * 32 + 8 * g + e) bad("fragment", KM ? "K outermost" : "rows outermost", C, i, lane, e);
+        if (got != (16 * (i >> 1) + r) * 64 + 32 * half + 8 * g + e) bad("fragment", KM ? "K outermost" : "rows outermost", C, i, lane, e);
         ++checks;
       }
     }
@@ -155,7 +159,7 @@ int main() {
   fragments<256, true>();
   for (int rows : {1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 613, 1500, 4096, 70001})
     for (int vocab : {1, 2, 31, 32, 33, 100, 255, 256, 257, 300, 513, 1024, 4099, 32001, 151936, 152064})
-      for (int hidden : {32, 64, 96, 128, 160, 256, 288, 1536, 3584})
-        sizes(rows, vocab, hidden, hidden % 64 ? 8 : 0);
+      for (int hidden : {64, 128, 192, 256, 320, 1536, 3584})
+        sizes(rows, vocab, hidden, hidden % 128 ? 8 : 0);
   std::printf("%lld checks\n", checks);
 }

@@ -90,7 +90,7 @@ HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stri
     ("rollout_head_logprobs", HEAD, dict(hidden_states=ARRAY + 8), "aligned"),
     ("rollout_head_logprobs", HEAD, dict(lm_head=None), "lm_head"),
     ("rollout_head_logprobs", HEAD, dict(lm_head=ARRAY + 2), "aligned"),
-    ("rollout_head_logprobs", HEAD, dict(hidden=48, hidden_stride=48, head_stride=48), "multiple of 32"),
+    ("rollout_head_logprobs", HEAD, dict(hidden=96, hidden_stride=96, head_stride=96), "multiple of 64"),
     ("rollout_head_logprobs", HEAD, dict(hidden_stride=68), "hidden_stride"),
     ("rollout_head_logprobs", HEAD, dict(hidden_stride=56), "hidden_stride"),
     ("rollout_head_logprobs", HEAD, dict(head_stride=(1 << 22) + 8), "head_stride"),
@@ -102,7 +102,7 @@ HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stri
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden_states=ARRAY + 8), "aligned"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(lm_head=None), "lm_head"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(lm_head=ARRAY + 2), "aligned"),
-    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden=48, hidden_stride=48, head_stride=48), "multiple of 32"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden=96, hidden_stride=96, head_stride=96), "multiple of 64"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden_stride=68), "hidden_stride"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(hidden_stride=56), "hidden_stride"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(head_stride=(1 << 22) + 8), "head_stride"),
