@@ -59,6 +59,7 @@ void launch_rows(const EmbedArgs& a, hipStream_t s) {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / WAVE;
 constexpr int kRange = 512;   // ids of a sorting workgroup at most: kSortWaves counters each are 32 KB of LDS
 constexpr int kChunk = 16;    // sorted rows of a summing workgroup
+constexpr int kFill = 8192;   // 16-byte vectors of the matrix that a filling workgroup writes
 
 struct EmbedSort {
   int* row;        // [n] rows sorted by id, equal ids in the order of the rows
@@ -93,8 +94,8 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, E
   if ((int)blockIdx.x >= ranges) {  // out = base, or 0
     if (!fill) return;
     constexpr int E = kVec<G>;
-    const long long total = (long long)a.vocab * a.hidden, threads = (long long)(gridDim.x - ranges) * kSortThreads;
-    const long long me = (long long)(blockIdx.x - ranges) * kSortThreads + tid;
+    const long long total = (long long)a.vocab * a.hidden;
+    const long long block = blockIdx.x - ranges, me = block * kSortThreads + tid;
     G* out = (G*)a.out;
     const G* base = (const G*)a.base;
     const G zero = narrow1(0.f, G{});
@@ -103,14 +104,18 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, E
     if (me < head) out[me] = base ? base[me] : zero;
     if (me < total - tail) out[tail + me] = base ? base[tail + me] : zero;
     u32x4* o = (u32x4*)(out + head);
+    const u32x4* b = (const u32x4*)(base + head);
     const u32x4 none = {0, 0, 0, 0};
+    const long long first = block * kFill + tid, end = min(vecs, (block + 1) * (long long)kFill);
     if (!base) {
-      for (long long i = me; i < vecs; i += threads) __builtin_nontemporal_store(none, o + i);
+#pragma unroll 4
+      for (long long i = first; i < end; i += kSortThreads) o[i] = none;
     } else if ((((size_t)base - (size_t)out) & 15) == 0) {
-      const u32x4* b = (const u32x4*)(base + head);
-      for (long long i = me; i < vecs; i += threads) o[i] = b[i];
+#pragma unroll 4
+      for (long long i = first; i < end; i += kSortThreads) o[i] = b[i];
     } else {
-      for (long long i = head + me; i < tail; i += threads) out[i] = base[i];
+      for (long long i = head + first * E; i < head + end * E; i += kSortThreads * E)
+        for (int e = 0; e < E; ++e) out[i + e] = base[i + e];
     }
     return;
   }
@@ -262,17 +267,19 @@ __global__ __launch_bounds__(64) void embed_join_kernel(EmbedGrad a, EmbedSort q
   constexpr int E = VEC ? 8 : 1;
   const int chunk = blockIdx.x, col = (blockIdx.y * 64 + threadIdx.x) * E;
   const int n = *q.n_inside, next = (chunk + 1) * kChunk;
-  if (next >= n || col >= a.hidden) return;
+  if (next >= n) return;
   const int id = q.id[next];
   if (q.id[next - 1] != id) return;                          // nothing crosses
   if (chunk > 0 && q.id[chunk * kChunk - 1] == id) return;   // it began earlier
-  int lo = next, hi = n;  // the end of the run: first place behind `next` with another id
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (q.id[mid] == id) lo = mid + 1;
-    else hi = mid;
+  int end = chunk;  // the last chunk that the run reaches: ids are sorted, so those at the chunks' first places tell
+  for (;;) {
+    const long long first = (long long)(end + 1 + (int)threadIdx.x % WAVE) * kChunk;
+    const unsigned long long in_run = __ballot(first < n && q.id[first < n ? first : 0] == id);
+    const int more = ~in_run ? __builtin_ctzll(~in_run) : WAVE;
+    end += more;
+    if (more < WAVE) break;
   }
-  const int end = (lo - 1) / kChunk;  // the chunk that holds its last row
+  if (col >= a.hidden) return;
   float sum[E];
   load_row<float, VEC, E>(q.last + (long long)chunk * a.hidden + col, sum);
 #pragma unroll 4
@@ -304,7 +311,7 @@ void launch_grad(const EmbedGrad& a, void* ws, hipStream_t s) {
   q.last = (float*)take((size_t)p.chunks * a.hidden * 4);
   const bool fill = a.base != a.out;
   const long long bytes = (long long)a.vocab * a.hidden * sizeof(G);
-  const int fillers = fill ? (int)std::min<long long>(1024, ceil_div(bytes, 64 << 10)) : 0;
+  const int fillers = fill ? ceil_div(bytes, kFill * 16) : 0;
   embed_sort_kernel<G><<<p.ranges + fillers, kSortThreads, 0, s>>>(a, q, p.ranges, p.range, fill);
   if (p.chunks == 0) return;
   // whole vectors of 8 values: every row starts on 16 bytes

@@ -337,8 +337,7 @@ __global__ __launch_bounds__(256) void head_finish_kernel(HeadArgs in, TokenOut 
   const float c = in.inv_temp * kLog2e;
   RowSums s{kLowest, 0.f, 0.f};
   for (int i = lane; i < parts; i += WAVE) s = merge(s, sums[(long long)row * parts + i], c);
-#pragma unroll
-  for (int o = 1; o < WAVE; o <<= 1) s = merge(s, RowSums{__shfl_xor(s.m, o, WAVE), __shfl_xor(s.s, o, WAVE), __shfl_xor(s.t, o, WAVE)}, c);
+  s = merge_wave(s, c);
   if (lane) return;
   const int t = in.targets ? in.targets[row] : -1;
   const bool has = t >= 0 && t < in.vocab;

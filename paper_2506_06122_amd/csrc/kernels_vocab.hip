@@ -6,21 +6,24 @@
 // values is taken relative to the new maximum, the old sums are scaled once a chunk.  The pass is bound by memory; the
 // arithmetic (9 issue slots per value, the exponential counting four) comes next.
 //
-// Alternatives ride along for free: the K-th largest of the threads' maxima is a bound that K values reach, and every value
-// that reaches it sits with a thread whose maximum does.  So only those threads' values are read again, spread over the
-// workgroup, and what reaches the bound - a few more than K - is ranked.  Rows that defeat this (long runs of equal values,
-// NaN) are found one alternative per sweep instead.
+// Alternatives ride along: every thread notes the maximum of each of kSegments runs of its values.  The K-th largest of
+// these is a bound that K values reach, and every value that reaches it lies in a run whose maximum does.  So only those
+// runs are read again, spread over the workgroup, and what reaches the bound - a few more than K - is ranked.  Rows that
+// defeat this (long stretches of equal values, NaN) are found one alternative per sweep instead.
 //
 // A row belongs to one workgroup where rows are enough; fewer are cut into parts whose results a second launch joins.
 #include "vocab.h"
 #include "vocab_vec.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
 constexpr int T = kTokenThreads, NW = T / WAVE;
 constexpr int kListed = 1024;       // candidates a workgroup can rank
+constexpr int kSegments = 4;        // runs of a thread's vectors whose maxima are kept, where each has at least kRun vectors
+constexpr int kRun = 8;
 constexpr int kPartValues = 2048;   // fewest values worth a workgroup
 constexpr int kFill = 1024;         // workgroups that fill the card
 
@@ -65,49 +68,49 @@ struct RowSlice {
   __device__ int values() const { return head_here + (end - begin) * kVec<V> + tail; }
 };
 
-__device__ inline RowSums merge_wave(RowSums r, float c) {
-#pragma unroll
-  for (int o = 1; o < WAVE; o <<= 1)
-    r = merge(r, RowSums{__shfl_xor(r.m, o, WAVE), __shfl_xor(r.s, o, WAVE), __shfl_xor(r.t, o, WAVE)}, c);
-  return r;
-}
-
 struct TopShared {
-  unsigned max_key[T];
-  unsigned short hot[T];
+  unsigned max_key[kSegments * T];
+  unsigned short hot[kSegments * T];
   unsigned bound;
   int n_hot, n_listed;
   unsigned long long best[NW];
   unsigned long long listed[kListed];
 };
 
+// A key that K or a few more of the keys reach, as near to the K-th greatest as that takes; 0 where they are fewer.  One
+// wavefront, N keys to a lane.
+template <int N>
+__device__ inline unsigned bound_of(const unsigned* keys, int K, int lane) {
+  unsigned k[N], bound = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) k[i] = keys[lane + i * WAVE];
+  for (int bit = 31; bit >= 0; --bit) {
+    const unsigned trial = bound | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __popcll(__ballot(k[i] >= trial));
+    if (n >= K) bound = trial;
+    if (n >= K && n <= K + K / 4) break;
+  }
+  return bound;
+}
+
 // The K greatest keys of the slice, greatest first, through emit(rank, key); ranks past the slice's values get key 0.
-// top: the thread's own maximum (no value: has = false).
+// sh.max_key holds the maxima of the threads' `runs` runs of `steps` vectors, T apart.
 template <typename V, typename Emit>
-__device__ void top_of_slice(const RowSlice<V>& row, float top, bool has, int K, TopShared& sh, Emit&& emit) {
-  constexpr int E = kVec<V>;
+__device__ void top_of_slice(const RowSlice<V>& row, int runs, int steps, int K, TopShared& sh, Emit&& emit) {
+  constexpr int E = kVec<V>, U = 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  sh.max_key[tid] = has ? value_key(top) : 0;
   if (tid == 0) sh.n_hot = sh.n_listed = 0;
   __syncthreads();
   if (wave == 0) {
-    unsigned k[T / WAVE];
-#pragma unroll
-    for (int i = 0; i < T / WAVE; ++i) k[i] = sh.max_key[lane + i * WAVE];
-    unsigned bound = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-      const unsigned trial = bound | 1u << bit;
-      int n = 0;
-#pragma unroll
-      for (int i = 0; i < T / WAVE; ++i) n += __popcll(__ballot(k[i] >= trial));
-      if (n >= K) bound = trial;
-      if (n == K) break;
-    }
+    const unsigned bound = runs > 1 ? bound_of<kSegments * T / WAVE>(sh.max_key, K, lane) : bound_of<T / WAVE>(sh.max_key, K, lane);
     if (lane == 0) sh.bound = max(bound, 1u);
   }
   __syncthreads();
   const unsigned bound = sh.bound;
-  if (sh.max_key[tid] >= bound) sh.hot[atomicAdd(&sh.n_hot, 1)] = (unsigned short)tid;
+  for (int i = 0; i < runs; ++i)
+    if (sh.max_key[i * T + tid] >= bound) sh.hot[atomicAdd(&sh.n_hot, 1)] = (unsigned short)(i * T + tid);
   auto consider = [&](float x, int id) {
     const unsigned key = value_key(x);
     if (key >= bound) {
@@ -118,14 +121,28 @@ __device__ void top_of_slice(const RowSlice<V>& row, float top, bool has, int K,
   const int one = row.single(tid);
   if (one >= 0) consider(to_f32(row.x[one]), one);
   __syncthreads();
-  const int steps = (row.end - row.begin + T - 1) / T;
-  for (int w = tid; w < sh.n_hot * steps; w += T) {
-    const int i = row.begin + sh.hot[w / steps] + w % steps * T;
-    if (i >= row.end) continue;
-    float v[E];
-    widen(row.vec(i), v, V{});
+  // vector w of the runs to read: step w % steps of run hot[w / steps]; the quotient by a product is exact, since
+  // w + 1/2 is at least 1 / (2 steps) of it away from a whole number and w < 2^20
+  const int n_vecs = sh.n_hot * steps;
+  const float by = 1.0f / (float)steps;
+  for (int w0 = tid; w0 < n_vecs; w0 += U * T) {
+    u32x4 v4[U];
+    int at[U];
 #pragma unroll
-    for (int e = 0; e < E; ++e) consider(v[e], row.id(i) + e);
+    for (int u = 0; u < U; ++u) {
+      const int w = w0 + u * T, h = min((int)(((float)w + 0.5f) * by), sh.n_hot - 1), hot = sh.hot[h];
+      at[u] = row.begin + ((hot / T) * steps + w - h * steps) * T + hot % T;
+      if (w >= n_vecs || at[u] >= row.end) at[u] = -1;
+      else v4[u] = row.vec(at[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at[u] >= 0) {
+        float v[E];
+        widen(v4[u], v, V{});
+#pragma unroll
+        for (int e = 0; e < E; ++e) consider(v[e], row.id(at[u]) + e);
+      }
   }
   __syncthreads();
   const int n = sh.n_listed, want = min(K, row.values());
@@ -180,6 +197,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOu
   constexpr int E = kVec<V>, U = 4;
   __shared__ RowSums wave_s[NW];
   __shared__ float log_s_s;
+  __shared__ std::conditional_t<TOP, TopShared, int> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
   const RowSlice<V> row((const V*)in.logits + r * in.stride, in.vocab, part, p.parts);
@@ -189,35 +207,40 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOu
   const float x_target = has_target && p.parts == 1 ? to_f32(row.x[target]) : 0.f;
   // the reference starts at the lowest finite value: a row of -inf then has differences of -inf, not NaN
   RowSums sums{kLowest, 0.f, 0.f};
-  float single = -INFINITY;
   const int one = row.single(tid);
-  if (one >= 0) single = to_f32(row.x[one]);
-  int i = row.begin + tid;
-  for (; i + (U - 1) * T < row.end; i += U * T) {
-    u32x4 w[U];
-    float v[U * E];
+  const int vecs = row.end - row.begin, runs = TOP && vecs >= kSegments * kRun * T ? kSegments : 1;
+  const int steps = max(1, (vecs + runs * T - 1) / (runs * T));
+  for (int q = 0; q < runs; ++q) {
+    int i = row.begin + q * steps * T + tid;
+    const int end = min(row.end, row.begin + (q + 1) * steps * T);
+    const bool has = i < end;
+    float top = -INFINITY;
+    for (; i + (U - 1) * T < end; i += U * T) {
+      u32x4 w[U];
+      float v[U * E];
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = row.vec(i + u * T);
+      for (int u = 0; u < U; ++u) w[u] = row.vec(i + u * T);
 #pragma unroll
-    for (int u = 0; u < U; ++u) widen(w[u], v + u * E, V{});
-    add_chunk<U * E>(sums, v, c);
-  }
-  const bool has = one >= 0 || row.begin + tid < row.end;
-  {
-    u32x4 w[U];
-    float v[U * E];
+      for (int u = 0; u < U; ++u) widen(w[u], v + u * E, V{});
+      top = fmaxf(top, add_chunk<U * E>(sums, v, c));
+    }
+    u32x4 w[U - 1];
+    float v[E];
 #pragma unroll
     for (int u = 0; u < U - 1; ++u)
-      if (i + u * T < row.end) w[u] = row.vec(i + u * T);
+      if (i + u * T < end) w[u] = row.vec(i + u * T);
 #pragma unroll
     for (int u = 0; u < U - 1; ++u)
-      if (i + u * T < row.end) {
+      if (i + u * T < end) {
         widen(w[u], v, V{});
-        add_chunk<E>(sums, v, c);
+        top = fmaxf(top, add_chunk<E>(sums, v, c));
       }
-    if (one >= 0) add_chunk<1>(sums, &single, c);
+    if constexpr (TOP) sh.max_key[q * T + tid] = has ? value_key(top) : 0;
   }
-  // (what starts at the lowest finite value stays there when every value is -inf; both order alike below any other)
+  if (one >= 0) {
+    const float x = to_f32(row.x[one]);
+    add_chunk<1>(sums, &x, c);
+  }
   const RowSums all = merge_wave(sums, c);
   if (lane == 0) wave_s[wave] = all;
   __syncthreads();
@@ -230,12 +253,9 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOu
     p.sums[(long long)r * p.parts + part] = total;
   }
   if constexpr (TOP) {
-    __shared__ TopShared sh;
     __syncthreads();
     const float log_s = p.parts == 1 ? log_s_s : 0.f;
-    // a maximum that is still the start stands for -inf: the bound must not lie above the values themselves
-    const float top = sums.m == kLowest ? -INFINITY : sums.m;
-    top_of_slice(row, top, has, out.top, sh, [&](int rank, unsigned long long key) {
+    top_of_slice(row, runs, steps, out.top, sh, [&](int rank, unsigned long long key) {
       if (p.parts == 1) store_top(out, r, rank, key, total.m, log_s, in.inv_temp);
       else p.keys[((long long)r * p.parts + part) * out.top + rank] = key;
     });
@@ -266,9 +286,10 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
   for (int w = 1; w < NW; ++w) total = merge(total, wave_s[w], c);
   if (tid == 0) log_s_s = finish_row(total, out, r, has_target, x_target, in.inv_temp);
   if constexpr (TOP) {
-    // Of every part's `deep` greatest keys the last: the `wide`-th greatest of these is a bound that K keys reach
+    // Of every part's `deep` greatest keys the last: the `wide`-th greatest of these is a bound that K keys reach, and
+    // with about half the parts above it few more do
     const unsigned long long* keys = p.keys + (long long)r * p.parts * out.top;
-    const int deep = (out.top + p.parts - 1) / p.parts, wide = (out.top + deep - 1) / deep;
+    const int deep = (2 * out.top + p.parts - 1) / p.parts, wide = (out.top + deep - 1) / deep;
     if (wave == 0) {
       const unsigned long long key = lane < p.parts ? keys[(long long)lane * out.top + deep - 1] : 0;
       int rank = 0;

@@ -92,13 +92,14 @@ __device__ inline RowSums merge(const RowSums& p, const RowSums& q, float c) {
   const float fp = __builtin_amdgcn_exp2f(-dp), fq = __builtin_amdgcn_exp2f(-dq);
   return RowSums{m, p.s * fp + q.s * fq, (p.t - dp * p.s) * fp + (q.t - dq * q.s) * fq};
 }
-// N more values.  The quick form makes a NaN of 0 x -inf for values of -inf (and of anything the plain exponent
+// N more values; returns their maximum.  The quick form makes a NaN of 0 x -inf for values of -inf (and of anything the plain exponent
 // cannot hold): such chunks are summed again with care, and what is NaN or +inf among the values stays NaN.
 template <int N>
-__device__ inline void add_chunk(RowSums& r, const float* v, float c) {
-  float m = r.m;
+__device__ inline float add_chunk(RowSums& r, const float* v, float c) {
+  float top = v[0];
 #pragma unroll
-  for (int i = 0; i < N; ++i) m = fmaxf(m, v[i]);
+  for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+  const float m = fmaxf(r.m, top);
   const float d = raise(r.m, m, c), f = __builtin_amdgcn_exp2f(-d), ref = rintf(m * c);
   const float t0 = (r.t - d * r.s) * f, s0 = r.s * f;
   float s = s0, t = t0;
@@ -120,6 +121,29 @@ __device__ inline void add_chunk(RowSums& r, const float* v, float c) {
     }
   }
   r = RowSums{m, s, t};
+  return top;
+}
+
+// Over a wavefront without a trip through LDS; every lane gets the result.  The lanes' order is fixed.
+template <int CTRL, int ROWS = 0xf>
+__device__ inline float dpp(float v, float other) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(other), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+template <typename F>
+__device__ inline float across_wave(float v, float none, F&& f) {
+  v = f(v, dpp<0x111>(v, none));       // the lane 1 below in the row of 16, then 2, 4, 8
+  v = f(v, dpp<0x112>(v, none));
+  v = f(v, dpp<0x114>(v, none));
+  v = f(v, dpp<0x118>(v, none));
+  v = f(v, dpp<0x142, 0xa>(v, none));  // the last lane of the row before, into rows 1 and 3
+  v = f(v, dpp<0x143, 0xc>(v, none));  // lane 31 into rows 2 and 3
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ inline RowSums merge_wave(const RowSums& r, float c) {
+  const float m = across_wave(r.m, kLowest, [](float a, float b) { return fmaxf(a, b); });
+  const float d = raise(r.m, m, c), f = __builtin_amdgcn_exp2f(-d);
+  const auto add = [](float a, float b) { return a + b; };
+  return RowSums{m, across_wave(r.s * f, 0.f, add), across_wave((r.t - d * r.s) * f, 0.f, add)};
 }
 
 // A row's results from its sums, written by one thread; x_target is read only with a target.  Returns ln S.
