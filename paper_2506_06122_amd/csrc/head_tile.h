@@ -42,9 +42,12 @@ struct HeadSlice {
   }
 };
 
-// Workgroup -> tile.  Consecutive workgroups go to the eight XCDs in turn, each with an L2 of its own, so tiles go to an XCD in
-// groups of group_m x group_n that run side by side there and share their operands' slices; groups go round the XCDs, down
-// the rows first.
+// Workgroup -> tile.  Consecutive workgroups go to the eight XCDs in turn, each with an L2 of its own.  Tiles come in groups of
+// group_m x group_n that run side by side on an XCD and share their operands' slices.  Groups go down the rows first and
+// round the XCDs, so that what these fetch at a time lies together (grad_head of 4096 rows, 152064 x 3584: 2.9 ms;
+// across first, or each XCD a contiguous share, 3.3); with cuts of K each XCD takes a contiguous share, because the tiles
+// of a cut share all of its slices (grad_hidden of 1500 rows, 151936 x 2048, six cuts: round the XCDs 0.79 ms, in
+// shares 0.67).
 struct HeadGrid {
   int m_tiles, n_tiles, splits;
   int group_m, group_n, m_groups, n_groups;
@@ -73,10 +76,11 @@ constexpr HeadGrid head_grid_rows(HeadGrid g, int m_tiles) {
 }
 constexpr int head_blocks(const HeadGrid& g) { return head_up(g.m_groups * g.n_groups * g.splits, 8) * g.group_m * g.group_n; }
 constexpr HeadBlock head_block(unsigned index, const HeadGrid& g) {
-  const int per = g.group_m * g.group_n, idx = (int)(index >> 3), in = idx % per;
-  const int group = idx / per * 8 + (int)(index & 7), across = group / g.m_groups;
+  const int per = g.group_m * g.group_n, idx = (int)(index >> 3), in = idx % per, share = (g.m_groups * g.n_groups * g.splits + 7) / 8;
+  if (idx / per >= share) return HeadBlock{0, 0, 0, false};
+  const int group = g.splits > 1 ? (int)(index & 7) * share + idx / per : idx / per * 8 + (int)(index & 7);
+  const int across = group / g.m_groups, z = across / g.n_groups;
   const int m = group % g.m_groups * g.group_m + in % g.group_m, n = across % g.n_groups * g.group_n + in / g.group_m;
-  const int z = across / g.n_groups;
   return HeadBlock{m, n, z, m < g.m_tiles && n < g.n_tiles && z < g.splits};
 }
 
@@ -88,25 +92,91 @@ constexpr HeadTile head_tile(int M, int N) {
   if (M <= 16) return {16, 256};
   if (M <= 32) return {32, 256};
   if (M <= 64) return {64, 256};
-  if (head_ceil(M, 256) * (long long)head_ceil(N, 256) < 192) return {128, 128};
+  if (M <= 256 || head_ceil(M, 256) * (long long)head_ceil(N, 256) < 192) return {128, 128};
   return {256, 256};
 }
+// the gradients' first product writes whole slices of rows, zeros included (16 x 256 tiles, 7 rows: 208 us, four times the
+// workgroups)
+constexpr HeadTile head_tile_logits(int M, int N) { return head_tile(head_max(M, 64), N); }
+// the gradients' second and third product: K is long in grad_hidden's, which is cut along it instead, and short in
+// grad_head's with few rows, where two small workgroups to a CU hide each other's start and end (7 rows 498 -> 470 us
+// in all, 187 rows 600 -> 576, but 613 rows 900 -> 940)
+constexpr HeadTile head_tile_hidden(int M) { return M <= 256 ? HeadTile{128, 128} : HeadTile{256, 256}; }
+constexpr HeadTile head_tile_head(int K) { return K <= 256 ? HeadTile{128, 128} : HeadTile{256, 256}; }
 
+// Cuts of K for `tiles` tiles of a product with k_tiles slices: rounds over the card's places for workgroups, in slices.  A cut
+// costs the tile's partial results, written and read again, as much as some twenty slices of the largest tile.
+constexpr int head_splits(int tiles, int k_tiles, HeadTile t) {
+  const int places = t.m == 256 ? 256 : 512, cost = t.m == 256 ? 20 : 8;
+  int best = 1, best_time = head_ceil(tiles, places) * (k_tiles + cost);
+  for (int rounds = 1; rounds <= 4; ++rounds) {
+    const int s = head_min(places * rounds / tiles, k_tiles / 8);
+    if (s <= 1) continue;
+    const int time = head_ceil((long long)tiles * s, places) * (head_ceil(k_tiles, s) + cost);
+    if (time < best_time) {
+      best_time = time;
+      best = s;
+    }
+  }
+  return best;
+}
+
+// The gradients of the logits are bf16.  One rounding of the given token's, by far the row's largest, moves the whole row
+// of both results; over many rows that averages out to the size of the results' own rounding, with few it does not, and
+// the gradients are kept as a bf16 value and the bf16 rest, below the first values' rows: twice the rows for
+// grad_hidden's product, twice the K for grad_head's, which few rows do not notice much.
+constexpr int kHeadTwoPlanes = 128;  // rows up to which
 struct HeadGradPlan {
-  int rows;    // room for the rows of the logits' gradients: a whole number of k-tiles
+  int rows;    // room for the rows of the logits' gradients: a whole number of slices
+  int planes;  // 1 or 2
   int chunk;   // columns of the vocabulary at a time, a multiple of 256
-  int splits;  // of K in grad_hidden's product
 };
-constexpr HeadGradPlan head_grad_plan(int rows, int vocab, int hidden) {
+constexpr HeadGradPlan head_grad_plan(int rows, int vocab) {
   HeadGradPlan g{};
   g.rows = head_up(head_max(rows, 1), kHeadDeep);
+  g.planes = rows <= kHeadTwoPlanes ? 2 : 1;
   // up to 4 GiB of gradients of logits at a time
-  const long long fit = ((long long)4 << 30) / (2ll * g.rows) / 256 * 256, all = head_up(vocab, 256);
+  const long long fit = ((long long)4 << 30) / (2ll * g.rows * g.planes) / 256 * 256, all = head_up(vocab, 256);
   g.chunk = (int)(fit < 256 ? 256 : fit < all ? fit : all);
-  const HeadTile t = head_tile(rows, hidden);
-  const int tiles = head_max(1, head_ceil(rows, t.m) * head_ceil(hidden, t.n));
-  g.splits = head_max(1, head_min(head_ceil(1024, tiles), g.chunk / 1024));
   return g;
+}
+// What `count` rows with a gradient make of it, known to the device only
+struct HeadActive {
+  int count;   // rows
+  int stacked; // rows of the logits' gradients as the products see them: the planes below each other, each a whole number
+               // of slices (zeros in between)
+  int splits;  // of K in grad_hidden's product
+};
+constexpr HeadActive head_active(int count, const HeadGradPlan& g, int vocab, int hidden) {
+  HeadActive a{count, g.planes == 1 ? count : 2 * head_up(count, kHeadDeep), 1};
+  // (the tile is chosen by the rows there is room for: the launch does not know the count)
+  const HeadTile t = head_tile_hidden(g.rows * g.planes);
+  const int tiles = head_ceil(a.stacked, t.m) * head_ceil(hidden, t.n), slices = head_ceil(head_min(vocab, g.chunk), kHeadDeep);
+  if (tiles > 0) a.splits = head_splits(tiles, slices, t);
+  return a;
+}
+// the most that any count needs: rows of partial results, and workgroups of grad_hidden's product
+struct HeadMost {
+  long long plane_rows;
+  int blocks;
+};
+constexpr HeadMost head_most(const HeadGradPlan& g, int rows, int vocab, int hidden) {
+  const HeadTile t = head_tile_hidden(g.rows * g.planes);
+  const int m_tiles = head_ceil(g.rows * g.planes, t.m);
+  const HeadGrid grid = head_grid(m_tiles, head_ceil(hidden, t.n), 1);
+  HeadMost most{0, 0};
+  // splits change with the number of row tiles alone; the last count of each has the most rows
+  for (int i = 1; i <= m_tiles; ++i) {
+    const int end = head_min(rows, g.planes == 1 ? i * t.m : i * t.m / 2);
+    const HeadActive a = head_active(head_max(end, 1), g, vocab, hidden);
+    HeadGrid some = head_grid_rows(grid, head_ceil(a.stacked, t.m));
+    some.splits = a.splits;
+    const long long plane_rows = (long long)a.splits * a.stacked;
+    if (plane_rows > most.plane_rows) most.plane_rows = plane_rows;
+    if (head_blocks(some) > most.blocks) most.blocks = head_blocks(some);
+    if (i > 600 && i < m_tiles - 1) i = m_tiles - 2;  // (far beyond that many tiles K is not cut)
+  }
+  return most;
 }
 // columns between the rows of a chunk's gradients: the padding of K in the product that follows, and of its tiles
 constexpr int head_grad_pitch(int columns) { return head_up(columns, 256); }

@@ -34,10 +34,8 @@ struct Operand {
 };
 struct Product {
   Operand a, b;
-  int M, N, K;          // b with K outermost has exactly K steps; anything else is padded to whole k-tiles
-  const int* count;     // device: where not NULL, M (or K, with `count_is_k`) is *count
-  bool count_is_k;
-  int splits, k_tiles_per_split;
+  int M, N, K;            // b with K outermost has exactly K steps; anything else is padded to whole slices
+  const HeadActive* plan; // device: TO_GRAD's M, TO_PLANE's M and cuts of K, TO_BF16's K
   HeadGrid grid;
   void* out;
   long long out_pitch;
@@ -50,7 +48,7 @@ struct Product {
   // TO_GRAD: rows of A are rows active[.] of the caller's arrays; columns start at col0 of the vocabulary
   const int* active;
   const float *row_stats, *entropy, *grad_logp, *grad_entropy;
-  int col0, vocab, row_capacity;
+  int col0, vocab, row_capacity, planes;
 };
 
 __device__ __forceinline__ void load_to_lds(unsigned lds, unsigned voff, const void* base) {
@@ -91,7 +89,7 @@ __device__ __forceinline__ u32x4 fragment(const char* slice, int i, int half, in
 // in order, later stages stay in flight), whose first half is read while the second is multiplied.  The copies past the
 // end of K repeat the last slice, so that every stage counts the same number of them.
 template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
-__global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_product_kernel(Product p) {
+__global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void head_product_kernel(Product p) {
   constexpr bool WIDE = MT * NT >= 32;
   constexpr int NW = WM * WN, BM = WM * MT * 16, BN = WN * NT * 16;
   using A = HeadSlice<BM, AK>;
@@ -105,12 +103,16 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
   __shared__ __attribute__((aligned(1024))) char lds[LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int M = p.count && !p.count_is_k ? *p.count : p.M, K = p.count && p.count_is_k ? *p.count : p.K;
-  const HeadBlock block = head_block(blockIdx.x, head_grid_rows(p.grid, head_ceil(TO == TO_GRAD ? head_up(M, kHeadDeep) : M, BM)));
+  const int M = TO == TO_GRAD ? p.plan->count : TO == TO_PLANE ? p.plan->stacked : p.M, K = TO == TO_BF16 ? p.plan->stacked : p.K;
+  HeadGrid grid = p.grid;
+  if constexpr (TO == TO_GRAD || TO == TO_PLANE) grid = head_grid_rows(grid, head_ceil(TO == TO_GRAD ? head_up(M, kHeadDeep) : M, BM));
+  if constexpr (TO == TO_PLANE) grid.splits = p.plan->splits;
+  const HeadBlock block = head_block(blockIdx.x, grid);
   if (!block.inside) return;
   const int bn = block.n, bz = block.z;
   const int m0 = block.m * BM, n0 = bn * BN;
-  const HeadExtent x = head_extent(AK, BK, TO == TO_GRAD, m0, n0, bz, M, p.N, K, p.k_tiles_per_split, p.a.pitch, p.row_capacity);
+  const HeadExtent x = head_extent(AK, BK, TO == TO_GRAD, m0, n0, bz, M, p.N, K, TO == TO_PLANE ? head_ceil(head_ceil(K, kHeadDeep), grid.splits) : head_ceil(K, kHeadDeep),
+                                   p.a.pitch, p.row_capacity);
   if (m0 >= x.m_end) return;
   const int k_tiles = x.k_tiles, kt_begin = x.kt_begin, kt_end = x.kt_end;
 
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int wm = wave / WN, wn = wave % WN;
-  if (kt_begin < kt_end) {
+  if (kt_begin < kt_end && m0 < M) {  // (rows of zeros that pad the next product's K take no product)
     // this wavefront's loads of a stage: units wave, wave + NW, ... of A's, then B's; their sources move on with the slices
     unsigned voff[L], tail[L], dst[L];
     bool is_b[L];
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
     for (int i = 0; i < MT; ++i) {
       const int m = m0 + (wm * MT + i) * 16 + r;
       if (m < M) {
-        f32x4* o = (f32x4*)((float*)p.out + ((long long)bz * p.M + m) * p.out_pitch);
+        f32x4* o = (f32x4*)((float*)p.out + ((long long)bz * M + m) * p.out_pitch);
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           const int n = col + j * 16;
@@ -309,23 +311,33 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 ? 1 : 2) void head_produ
               if (q.none || col + j * 16 + e >= p.N) acc[i][j][e] = 0.f;
         }
       }
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        uint2 w;
-        w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][0], acc[i][j][1]}), bf16_pair));
-        w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][2], acc[i][j][3]}), bf16_pair));
-        *(uint2*)(mine + (i * 16 + r) * OUT_ROW + j * 32 + g * 8) = w;
-      }
     }
-    // (only this wavefront's own writes are read: the compiler waits for them)
-    constexpr int LANES = NT * 2, ROWS = 64 / LANES;  // lanes to a row, rows at a time
     // columns that exist: the product's, or as far as the padding of K in the product that follows
+    constexpr int LANES = NT * 2, ROWS = 64 / LANES;  // lanes to a row, rows at a time
     const int n = col0 + lane % LANES * 8, n_end = TO == TO_GRAD ? (int)p.out_pitch : p.N;
+    uint16_t* out = (uint16_t*)p.out;
+    constexpr bool TWO = TO == TO_GRAD && BM <= 128;  // tiles of few rows
+#pragma unroll 1
+    for (int plane = 0; plane < (TWO ? p.planes : 1); ++plane) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          uint2 w;
+          w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][0], acc[i][j][1]}), bf16_pair));
+          w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{acc[i][j][2], acc[i][j][3]}), bf16_pair));
+          *(uint2*)(mine + (i * 16 + r) * OUT_ROW + j * 32 + g * 8) = w;
+          if constexpr (TWO)  // the rest
+            acc[i][j] -= f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+        }
+      // (only this wavefront's own writes are read: the compiler waits for them)
 #pragma unroll 4
-    for (int q = 0; q < MT * 16; q += ROWS) {
-      const int ml = q + lane / LANES, m = m0 + wm * MT * 16 + ml;
-      const u32x4 w = *(const u32x4*)(mine + ml * OUT_ROW + lane % LANES * 16);
-      if (m < x.m_end && n < n_end) *(u32x4*)((uint16_t*)p.out + m * p.out_pitch + n) = w;
+      for (int q = 0; q < MT * 16; q += ROWS) {
+        const int ml = q + lane / LANES, m = m0 + wm * MT * 16 + ml;
+        const u32x4 w = *(const u32x4*)(mine + ml * OUT_ROW + lane % LANES * 16);
+        if (m < x.m_end && n < n_end) *(u32x4*)(out + m * p.out_pitch + n) = w;
+      }
+      out += head_up(M, kHeadDeep) * p.out_pitch;
     }
   }
 }
@@ -345,8 +357,8 @@ __global__ __launch_bounds__(256) void head_finish_kernel(HeadArgs in, TokenOut 
 }
 
 // ---- rows that have a gradient ---------------------------------------------------------------
-// active[i] = i-th row with a gradient, place[row] = its i or -1, *count = their number.  One workgroup.
-__global__ __launch_bounds__(1024) void head_active_kernel(HeadGrad a, int* count, int* active, int* place) {
+// active[i] = i-th row with a gradient, place[row] = its i or -1, *plan = what follows from their number.  One workgroup.
+__global__ __launch_bounds__(1024) void head_active_kernel(HeadGrad a, HeadGradPlan g, HeadActive* plan, int* active, int* place) {
   __shared__ int wave_s[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int done = 0;
@@ -369,26 +381,43 @@ __global__ __launch_bounds__(1024) void head_active_kernel(HeadGrad a, int* coun
     done += all;
     __syncthreads();
   }
-  if (tid == 0) *count = done;
+  if (tid == 0) *plan = head_active(done, g, a.in.vocab, a.in.hidden);
 }
-// out[i] = hidden_states[active[i]], zeros behind them up to a whole k-tile; one row per workgroup
-__global__ __launch_bounds__(256) void head_gather_kernel(HeadArgs in, const int* count, const int* active, uint16_t* out) {
-  const int i = blockIdx.x, n = *count;
-  if (i >= head_up(n, kHeadDeep)) return;
+// The rows of hidden_states that go with the stacked gradients, zeros in between; one row per workgroup
+__global__ __launch_bounds__(256) void head_gather_kernel(HeadArgs in, int planes, const HeadActive* plan, const int* active, uint16_t* out) {
+  const int n = plan->count, rows = head_up(n, kHeadDeep), row = blockIdx.x;
+  if (row >= rows * planes) return;
+  const int i = row >= rows ? row - rows : row;
   const u32x4* src = i < n ? (const u32x4*)((const uint16_t*)in.hidden_states + active[i] * in.hidden_stride) : nullptr;
-  u32x4* dst = (u32x4*)(out + (long long)i * in.hidden);
+  u32x4* dst = (u32x4*)(out + (long long)row * in.hidden);
   const u32x4 zero = {0, 0, 0, 0};
   for (int v = threadIdx.x; v < in.hidden / 8; v += 256) dst[v] = src ? src[v] : zero;
 }
-// grad_hidden[row] = sum of the planes' row place[row], in their order; zeros where the row has none
-__global__ __launch_bounds__(256) void head_planes_kernel(const float* planes, int splits, int rows, int hidden, const int* place, uint16_t* out) {
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int per_row = hidden / 4, row = (int)(at / per_row), col = (int)(at % per_row) * 4;
-  if (row >= rows) return;
-  const int i = place[row];
+// grad_hidden[row] = sum over the cuts of K of the rows that go with place[row]; zeros where it has none.  A workgroup takes 64 quads of columns, a
+// wavefront a quarter of the planes, in their order; the quarters meet in LDS.
+__global__ __launch_bounds__(256) void head_planes_kernel(const float* part_rows, int planes, const HeadActive* plan, int rows, int hidden, const int* place, uint16_t* out) {
+  __shared__ f32x4 part[3][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per_row = hidden / 4;
+  const long long at = (long long)blockIdx.x * 64 + lane;
+  const int row = (int)min(at / per_row, (long long)rows - 1), col = (int)(at % per_row) * 4;
+  const int stacked = plan->stacked, second = planes == 2 ? stacked / 2 : 0;
+  const int i = place[row], splits = plan->splits, share = (splits + 3) / 4, end = min(splits, (wave + 1) * share);
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  if (i >= 0)
-    for (int z = 0; z < splits; ++z) s += *(const f32x4*)(planes + ((long long)z * rows + i) * hidden + col);
+  if (i >= 0) {
+#pragma unroll 8
+    for (int z = wave * share; z < end; ++z) {
+      const float* at_row = part_rows + ((long long)z * stacked + i) * hidden + col;
+      s += *(const f32x4*)at_row;
+      if (second) s += *(const f32x4*)(at_row + (long long)second * hidden);
+    }
+  }
+  if (wave) part[wave - 1][lane] = s;
+  __syncthreads();
+  if (wave || at >= (long long)rows * per_row) return;
+  s += part[0][lane];
+  s += part[1][lane];
+  s += part[2][lane];
   uint2 w;
   w.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{s[0], s[1]}), bf16_pair));
   w.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32_pair{s[2], s[3]}), bf16_pair));
@@ -397,19 +426,23 @@ __global__ __launch_bounds__(256) void head_planes_kernel(const float* planes, i
 
 // ---- shapes ------------------------------------------------------------------------------------
 template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
-void launch_shape(Product p, hipStream_t s) {
-  p.grid = head_grid(head_ceil(TO == TO_GRAD ? p.row_capacity : p.M, WM * MT * 16), head_ceil(p.N, WN * NT * 16), p.splits);
-  p.k_tiles_per_split = head_ceil(head_ceil(p.K, kHeadDeep), p.splits);
-  head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK><<<head_blocks(p.grid), WM * WN * 64, 0, s>>>(p);
+void launch_shape(Product p, int blocks, hipStream_t s) {
+  p.grid = head_grid(head_ceil(TO == TO_GRAD ? p.row_capacity : p.M, WM * MT * 16), head_ceil(p.N, WN * NT * 16), 1);
+  head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK><<<blocks ? blocks : head_blocks(p.grid), WM * WN * 64, 0, s>>>(p);
 }
+static_assert(kHeadTwoPlanes <= 256, "two planes leave tiles of up to 128 rows");
 template <int TO, bool AK, bool BK>
-void launch_product(const Product& p, hipStream_t s) {
-  const HeadTile t = head_tile(p.M, p.N);
-  if (t.m == 16) launch_shape<1, 4, 1, 4, 2, TO, AK, BK>(p, s);
-  else if (t.m == 32) launch_shape<1, 4, 2, 4, 2, TO, AK, BK>(p, s);
-  else if (t.m == 64) launch_shape<1, 4, 4, 4, 2, TO, AK, BK>(p, s);
-  else if (t.m == 128) launch_shape<2, 2, 4, 4, 2, TO, AK, BK>(p, s);
-  else launch_shape<2, 2, 8, 8, 2, TO, AK, BK>(p, s);
+void launch_product(const Product& p, HeadTile t, int blocks, hipStream_t s) {
+  if (t.m == 256) return launch_shape<2, 2, 8, 8, 2, TO, AK, BK>(p, blocks, s);
+  if (t.m == 128) return launch_shape<2, 2, 4, 4, 2, TO, AK, BK>(p, blocks, s);
+  if constexpr (!BK) {  // products that walk over W by its rows
+    if (t.m == 64) return launch_shape<1, 4, 4, 4, 2, TO, AK, BK>(p, blocks, s);
+    if constexpr (TO == TO_SUMS) {
+      if (t.m == 32) return launch_shape<1, 4, 2, 4, 2, TO, AK, BK>(p, blocks, s);
+      // three stages in flight in one workgroup per CU, 16 x 152064 x 3584 211 us; two stages and two workgroups 236
+      return launch_shape<1, 4, 1, 4, 3, TO, AK, BK>(p, blocks, s);
+    }
+  }
 }
 
 constexpr size_t piece(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
@@ -421,43 +454,46 @@ size_t head_workspace(int rows, int vocab, int) {
   return piece((size_t)rows * 4) + (size_t)rows * ceil_div(vocab, t.n) * sizeof(RowSums);
 }
 void launch_head_logprobs(const HeadArgs& in, const TokenOut& out, void* ws, hipStream_t s) {
+  const HeadTile t = head_tile(in.rows, in.vocab);
   Product p{};
   p.a = {in.hidden_states, in.hidden_stride};
   p.b = {in.lm_head, in.head_stride};
   p.M = in.rows;
   p.N = in.vocab;
   p.K = in.hidden;
-  p.splits = 1;
   p.inv_temp = in.inv_temp;
   p.targets = in.targets;
   p.target_logit = (float*)ws;
   p.sums = (RowSums*)((char*)ws + piece((size_t)in.rows * 4));
-  launch_product<TO_SUMS, false, false>(p, s);
-  head_finish_kernel<<<ceil_div(in.rows, 4), 256, 0, s>>>(in, out, p.sums, p.target_logit, ceil_div(in.vocab, head_tile(in.rows, in.vocab).n));
+  launch_product<TO_SUMS, false, false>(p, t, 0, s);
+  head_finish_kernel<<<ceil_div(in.rows, 4), 256, 0, s>>>(in, out, p.sums, p.target_logit, ceil_div(in.vocab, t.n));
 }
 
 size_t head_grad_workspace(int rows, int vocab, int hidden) {
-  const HeadGradPlan g = head_grad_plan(rows, vocab, hidden);
-  return piece(4) + 2 * piece((size_t)rows * 4) + piece((size_t)g.rows * hidden * 2) + piece((size_t)g.rows * g.chunk * 2) +
-         piece((size_t)g.splits * rows * hidden * 4);
+  const HeadGradPlan g = head_grad_plan(rows, vocab);
+  const size_t room = (size_t)g.rows * g.planes;
+  return piece(sizeof(HeadActive)) + 2 * piece((size_t)rows * 4) + piece(room * hidden * 2) + piece(room * g.chunk * 2) +
+         piece((size_t)head_most(g, rows, vocab, hidden).plane_rows * hidden * 4);
 }
 void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
   const HeadArgs& in = a.in;
-  const HeadGradPlan g = head_grad_plan(in.rows, in.vocab, in.hidden);
+  const HeadGradPlan g = head_grad_plan(in.rows, in.vocab);
+  const HeadMost most = head_most(g, in.rows, in.vocab, in.hidden);
+  const size_t room = (size_t)g.rows * g.planes;
   char* at = (char*)ws;
   auto take = [&](size_t bytes) {
     void* r = at;
     at += piece(bytes);
     return r;
   };
-  int* count = (int*)take(4);
+  HeadActive* plan = (HeadActive*)take(sizeof(HeadActive));
   int* active = (int*)take((size_t)in.rows * 4);
   int* place = (int*)take((size_t)in.rows * 4);
-  uint16_t* h = (uint16_t*)take((size_t)g.rows * in.hidden * 2);
-  uint16_t* dx = (uint16_t*)take((size_t)g.rows * g.chunk * 2);
-  float* planes = (float*)take((size_t)g.splits * in.rows * in.hidden * 4);
-  head_active_kernel<<<1, 1024, 0, s>>>(a, count, active, place);
-  head_gather_kernel<<<g.rows, 256, 0, s>>>(in, count, active, h);
+  uint16_t* h = (uint16_t*)take(room * in.hidden * 2);
+  uint16_t* dx = (uint16_t*)take(room * g.chunk * 2);
+  float* part_rows = (float*)at;
+  head_active_kernel<<<1, 1024, 0, s>>>(a, g, plan, active, place);
+  head_gather_kernel<<<(int)room, 256, 0, s>>>(in, g.planes, plan, active, h);
   for (int v0 = 0; v0 < in.vocab; v0 += g.chunk) {
     const int v = std::min(g.chunk, in.vocab - v0);
     const uint16_t* w = (const uint16_t*)in.lm_head + v0 * in.head_stride;
@@ -468,8 +504,7 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
       p.M = in.rows;
       p.N = v;
       p.K = in.hidden;
-      p.count = count;
-      p.splits = 1;
+      p.plan = plan;
       p.out = dx;
       p.out_pitch = head_grad_pitch(v);
       p.inv_temp = in.inv_temp;
@@ -482,34 +517,31 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
       p.col0 = v0;
       p.vocab = in.vocab;
       p.row_capacity = g.rows;
-      launch_product<TO_GRAD, false, false>(p, s);
+      p.planes = g.planes;
+      launch_product<TO_GRAD, false, false>(p, head_tile_logits(in.rows, v), 0, s);
       Product q{};  // + dx W
       q.a = {dx, p.out_pitch};
       q.b = {w, in.head_stride};
-      q.M = in.rows;
+      q.M = (int)room;
       q.N = in.hidden;
       q.K = v;
-      q.count = count;
-      q.splits = std::min(g.splits, std::max(1, head_ceil(v, kHeadDeep)));
-      q.out = planes;
+      q.plan = plan;
+      q.out = part_rows;
       q.out_pitch = in.hidden;
       q.add = v0 > 0;
-      launch_product<TO_PLANE, false, true>(q, s);
+      launch_product<TO_PLANE, false, true>(q, head_tile_hidden((int)room), most.blocks, s);
     }
     Product q{};  // dx^T h
     q.a = {dx, head_grad_pitch(v)};
     q.b = {h, in.hidden};
     q.M = v;
     q.N = in.hidden;
-    q.K = g.rows;
-    q.count = count;
-    q.count_is_k = true;
-    q.splits = 1;
+    q.plan = plan;
     q.out = (uint16_t*)a.grad_head + (long long)v0 * in.hidden;
     q.out_pitch = in.hidden;
-    launch_product<TO_BF16, true, true>(q, s);
+    launch_product<TO_BF16, true, true>(q, head_tile_head(in.rows), 0, s);
   }
   if (in.rows > 0)
-    head_planes_kernel<<<ceil_div((long long)in.rows * (in.hidden / 4), 256), 256, 0, s>>>(planes, g.splits, in.rows, in.hidden, place,
-                                                                                    (uint16_t*)a.grad_hidden);
+    head_planes_kernel<<<ceil_div((long long)in.rows * (in.hidden / 4), 64), 256, 0, s>>>(part_rows, g.planes, plan, in.rows, in.hidden, place,
+                                                                                   (uint16_t*)a.grad_hidden);
 }

@@ -19,13 +19,12 @@ struct Array {
 };
 struct Product {
   const char* name;
+  HeadTile tile;
   bool pad_rows;
   Array a, b, out;
   long long a_pitch, b_pitch, out_pitch, out_size;
-  int M, N, K, capacity, splits;
-  int count;       // what the device finds, -1: nothing
-  bool count_is_k;
-  long long plane_rows;
+  int m_room, M, N, K, capacity, splits, blocks;  // M, K, splits: as the device finds them
+  long long out_row;                              // rows before the first one's
 };
 
 template <int C, bool KM>
@@ -43,15 +42,16 @@ static void loads(const char* name, long long base, int limit, int k_left, long 
 
 template <int BM, int BN, bool AK, bool BK>
 static void walk(const Product& p) {
-  const int m_tiles = head_ceil(p.pad_rows ? p.capacity : p.M, BM), n_tiles = head_ceil(p.N, BN), per = head_ceil(head_ceil(p.K, kHeadDeep), p.splits);
-  const int tiles = m_tiles * n_tiles * p.splits, M = p.count >= 0 && !p.count_is_k ? p.count : p.M, K = p.count >= 0 && p.count_is_k ? p.count : p.K;
-  if (tiles < 20000) {
+  const int M = p.M, K = p.K, per = p.splits > 1 ? head_ceil(head_ceil(K, kHeadDeep), p.splits) : head_ceil(K, kHeadDeep);
+  const HeadGrid room = head_grid(head_ceil(p.pad_rows ? p.capacity : p.m_room, BM), head_ceil(p.N, BN), 1);
+  const int m_tiles = head_ceil(p.pad_rows ? head_up(M, kHeadDeep) : M, BM), n_tiles = room.n_tiles, tiles = m_tiles * n_tiles * p.splits;
+  const int blocks = p.blocks ? p.blocks : head_blocks(room);
+  HeadGrid grid = head_grid_rows(room, m_tiles);
+  grid.splits = p.splits;
+  if (head_blocks(grid) > blocks) bad("too few workgroups", p.name, head_blocks(grid), blocks, m_tiles, p.splits);
+  if (blocks < 200000) {
     std::vector<char> seen(tiles, 0);
-    const HeadGrid whole = head_grid(m_tiles, n_tiles, p.splits);
-    for (int some = 1; some <= m_tiles; some += 1 + m_tiles / 7)
-      if (head_blocks(head_grid_rows(whole, some)) > head_blocks(whole)) bad("more workgroups", p.name, some, m_tiles, n_tiles, p.splits);
-    const HeadGrid grid = head_grid_rows(whole, m_tiles);
-    for (int i = 0; i < head_blocks(grid); ++i) {
+    for (int i = 0; i < blocks; ++i) {
       const HeadBlock b = head_block(i, grid);
       if (!b.inside) continue;
       if (b.m < 0 || b.m >= m_tiles || b.n >= n_tiles || b.z >= p.splits || seen[(b.z * n_tiles + b.n) * m_tiles + b.m]++) bad("tile twice", p.name, i, b.m, b.n, b.z);
@@ -59,9 +59,9 @@ static void walk(const Product& p) {
     for (char c : seen)
       if (!c) bad("tile missing", p.name, tiles, 0, 0, 0);
   }
+  if (!m_tiles) return;
   std::set<int> ms{0, m_tiles / 2, m_tiles - 1, head_max(0, m_tiles - 2)}, ns{0, n_tiles - 1}, zs{0, p.splits / 2, p.splits - 1};
-  for (int i = 0; i < m_tiles; ++i)  // tiles around the end of the rows that the device finds
-    if (M / BM >= i - 1 && M / BM <= i + 1) ms.insert(i);
+  for (int i = head_max(0, M / BM - 1); i < head_min(m_tiles, M / BM + 2); ++i) ms.insert(i);  // around the end of the rows
   for (int m : ms)
     for (int n : ns)
       for (int z : zs) {
@@ -69,7 +69,7 @@ static void walk(const Product& p) {
         const HeadExtent x = head_extent(AK, BK, p.pad_rows, m0, n0, z, M, p.N, K, per, p.a_pitch, p.capacity);
         if (m0 >= x.m_end) continue;
         std::set<int> kts;
-        if (x.kt_begin < x.kt_end) kts = {x.kt_begin, x.kt_end - 1, (x.kt_begin + x.kt_end) / 2};
+        if (x.kt_begin < x.kt_end && m0 < M) kts = {x.kt_begin, x.kt_end - 1, (x.kt_begin + x.kt_end) / 2};
         for (int kt : kts) {
           const long long a0 = 2 * (AK ? m0 + kt * kHeadDeep * p.a_pitch : m0 * p.a_pitch + kt * kHeadDeep), b0 = 2 * (BK ? n0 + kt * kHeadDeep * p.b_pitch : n0 * p.b_pitch + kt * kHeadDeep);
           loads<BM, AK>(p.name, a0, x.a_limit, kHeadDeep, p.a_pitch, p.a);
@@ -78,14 +78,14 @@ static void walk(const Product& p) {
         // stores of four values: last row of the tile, last column that passes the kernel's test
         const int row = head_min(m0 + BM, x.m_end) - 1;
         const int cols = p.pad_rows ? (int)p.out_pitch : p.N, col = head_min(n0 + BN, cols) - 4;
-        const long long at = ((z * p.plane_rows + row) * p.out_pitch + col) * p.out_size;
+        const long long at = ((p.splits > 1 ? (long long)z * M + row : p.out_row + row) * p.out_pitch + col) * p.out_size;
         if (p.out.bytes && (at < 0 || at + 4 * p.out_size > p.out.bytes)) bad("store out of range", p.name, row, col, at, p.out.bytes);
         ++checks;
       }
 }
 template <bool AK, bool BK>
 static void by_tile(const Product& p) {
-  const HeadTile t = head_tile(p.M, p.N);
+  const HeadTile t = p.tile;
   if (t.m == 16 && t.n == 256) walk<16, 256, AK, BK>(p);
   else if (t.m == 32 && t.n == 256) walk<32, 256, AK, BK>(p);
   else if (t.m == 64 && t.n == 256) walk<64, 256, AK, BK>(p);
@@ -97,20 +97,26 @@ static void by_tile(const Product& p) {
 static void sizes(int rows, int vocab, int hidden, int pad) {
   const long long hp = hidden + pad;
   const Array states{(rows - 1) * hp * 2 + hidden * 2}, head{(vocab - 1) * hp * 2 + hidden * 2ll};
-  const HeadTile t = head_tile(rows, vocab);
-  by_tile<false, false>({"logits", false, states, head, {0}, hp, hp, 0, 0, rows, vocab, hidden, 0, 1, -1, false, 0});
-  if (head_ceil(vocab, t.n) < 1) bad("no parts", "logits", vocab, t.n, 0, 0);
-  const HeadGradPlan g = head_grad_plan(rows, vocab, hidden);
-  const Array h{(long long)g.rows * hidden * 2}, dx{(long long)g.rows * g.chunk * 2}, planes{(long long)g.splits * rows * hidden * 4};
-  for (int count : {0, 1, rows / 3, rows / 2 + 1, rows - 1, rows}) {
+  by_tile<false, false>({"logits", head_tile(rows, vocab), false, states, head, {0}, hp, hp, 0, 0, rows, rows, vocab, hidden, 0, 1, 0, 0});
+  const HeadGradPlan g = head_grad_plan(rows, vocab);
+  const HeadMost most = head_most(g, rows, vocab, hidden);
+  const int room = g.rows * g.planes;
+  const Array h{(long long)room * hidden * 2}, dx{(long long)room * g.chunk * 2}, parts{most.plane_rows * hidden * 4};
+  std::set<int> counts{0, 1, rows / 5, rows / 3, rows / 2 + 1, rows - 1, rows};
+  for (int c = 0; c < rows && c < 700; c += 64) counts.insert({c, c + 1});
+  for (int count : counts) {
     if (count < 0 || count > rows) continue;
+    const HeadActive a = head_active(count, g, vocab, hidden);
+    if (a.stacked > room || a.splits < 1) bad("plan", "active", count, a.stacked, room, a.splits);
     for (int v0 = 0; v0 < vocab; v0 += g.chunk) {
       const int v = head_min(g.chunk, vocab - v0), pitch = head_grad_pitch(v);
       if (pitch > g.chunk || pitch % 256 || pitch < v) bad("pitch", "gradients", pitch, g.chunk, v, 0);
       const Array w{(long long)(v - 1) * hp * 2 + hidden * 2ll + (long long)(vocab - v0 - v) * hp * 2};
-      by_tile<false, false>({"gradients", true, h, w, dx, hidden, hp, pitch, 2, rows, v, hidden, g.rows, 1, count, false, 0});
-      by_tile<false, true>({"grad_hidden", false, dx, w, planes, pitch, hp, hidden, 4, rows, hidden, v, 0, head_min(g.splits, head_ceil(v, kHeadDeep)), count, false, rows});
-      by_tile<true, true>({"grad_head", false, dx, h, {(long long)v * hidden * 2}, pitch, hidden, hidden, 2, v, hidden, g.rows, 0, 1, count, true, 0});
+      for (int plane = 0; plane < g.planes; ++plane)
+        by_tile<false, false>({"gradients", head_tile_logits(rows, v), true, h, w, dx, hidden, hp, pitch, 2, rows, count, v, hidden, g.rows, 1, 0,
+                               (long long)plane * head_up(count, kHeadDeep)});
+      by_tile<false, true>({"grad_hidden", head_tile_hidden(room), false, dx, w, parts, pitch, hp, hidden, 4, room, a.stacked, hidden, v, 0, a.splits, most.blocks, 0});
+      by_tile<true, true>({"grad_head", head_tile_head(rows), false, dx, h, {(long long)v * hidden * 2}, pitch, hidden, hidden, 2, v, v, hidden, a.stacked, 0, 1, 0, 0});
     }
   }
 }
@@ -158,8 +164,8 @@ int main() {
   fragments<128, true>();
   fragments<256, true>();
   for (int rows : {1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 613, 1500, 4096, 70001})
-    for (int vocab : {1, 2, 31, 32, 33, 100, 255, 256, 257, 300, 513, 1024, 4099, 32001, 151936, 152064})
-      for (int hidden : {64, 128, 192, 256, 320, 1536, 3584})
+    for (int vocab : {1, 33, 100, 256, 257, 513, 4099, 32001, 152064})
+      for (int hidden : {64, 192, 1536, 3584})
         sizes(rows, vocab, hidden, hidden % 128 ? 8 : 0);
   std::printf("%lld checks\n", checks);
 }
