@@ -6,6 +6,7 @@ tensors and their data pointers handed to rollout_init) and of the stream.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -499,38 +500,57 @@ def _refuse(msg):
     raise RolloutError(E_INVAL, msg)
 
 
-def _dtype_id(t, name):
+def _dtype_ids():
     import torch
-    ids = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
-    if t.dtype not in ids:
+    return {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+
+
+_dtype_table = None
+
+
+def _dtype_id(t, name):
+    global _dtype_table
+    if _dtype_table is None:
+        _dtype_table = _dtype_ids()
+    got = _dtype_table.get(t.dtype)
+    if got is None:
         _refuse(f"{name} must be float32, bfloat16 or float16")
-    return ids[t.dtype]
+    return got
 
 
 def _rows(t, name, device, dtype=None, shape=None):
     """A matrix on `device` whose rows lie anywhere, their values side by side.  Returns its row stride."""
-    if t.dim() != 2 or t.device != device or not t.is_cuda:
+    if t.dim() != 2 or not t.is_cuda or t.device != device:
         _refuse(f"{name} must be a matrix on the GPU that holds the other arrays")
     if dtype is not None and t.dtype != dtype:
         _refuse(f"{name} must be {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        _refuse(f"{name} must have shape {tuple(shape)}")
     rows, width = t.shape
-    if width > 1 and t.stride(1) != 1:
+    if shape is not None and (rows, width) != tuple(shape):
+        _refuse(f"{name} must have shape {tuple(shape)}")
+    step, one = t.stride()
+    if width > 1 and one != 1:
         _refuse(f"{name}: values of a row must be consecutive")
     if rows <= 1:
         return width
-    if t.stride(0) < width:
+    if step < width:
         _refuse(f"{name}: rows overlap")
-    return t.stride(0)
+    return step
 
 
 def _vector(t, name, device, dtype, n):
     if t is None:
         return None
-    if t.device != device or t.dtype != dtype or t.dim() != 1 or len(t) != n or not t.is_contiguous():
+    if t.dtype != dtype or t.dim() != 1 or len(t) != n or t.device != device or not t.is_contiguous():
         _refuse(f"{name} must be a contiguous {dtype} vector of {n} on {device}")
     return t.data_ptr()
+
+
+def _current_stream(device):
+    """Handle of the device's current PyTorch stream; asked for without building a Stream object where PyTorch offers that
+    (2 of a small call's 9 us)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 class _On:
@@ -539,12 +559,14 @@ class _On:
 
     def __init__(self, device, stream):
         import torch
-        self.guards = []
+        self.guards = ()
         if torch.cuda.current_device() != device.index:
-            self.guards.append(torch.cuda.device(device))
+            self.guards += (torch.cuda.device(device),)
         if stream is not None:
-            self.guards.append(torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)))
-        self.handle = stream if stream is not None else torch.cuda.current_stream(device).cuda_stream
+            self.guards += (torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)),)
+            self.handle = stream
+        else:
+            self.handle = _current_stream(device)
 
     def __enter__(self):
         for g in self.guards:
@@ -561,12 +583,23 @@ def _enqueued(lib, rc):
         raise RolloutError(rc, lib.rollout_last_error(None).decode())
 
 
-def _workspace(lib, size, device):
-    """Bytes for one call, from PyTorch's allocator: a graph under capture gets its own."""
-    import torch
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(name, *sizes):
+    lib = load_library()
+    size = getattr(lib, name)(*sizes)
     if size < 0:
         _enqueued(lib, size)
-    return torch.empty(size, dtype=torch.uint8, device=device) if size else None
+    return size
+
+
+def _workspace(name, device, *sizes):
+    """(address, bytes, tensor) of a workspace for one call, from PyTorch's allocator: a graph under capture gets its own."""
+    import torch
+    size = _workspace_bytes(name, *sizes)
+    if not size:
+        return None, 0, None
+    t = torch.empty(size, dtype=torch.uint8, device=device)
+    return t.data_ptr(), size, t
 
 
 def rollout_token_logprobs(logits, targets=None, *, temperature=1.0, top=0, stream=None):
@@ -581,14 +614,13 @@ def rollout_token_logprobs(logits, targets=None, *, temperature=1.0, top=0, stre
     dtype = _dtype_id(logits, "logits")
     tgt = _vector(targets, "targets", device, torch.int32, rows)
     with _On(device, stream) as s:
-        ws = _workspace(lib, lib.rollout_token_logprobs_workspace(rows, vocab, top), device)
-        logp, entropy = torch.empty(rows, device=device), torch.empty(rows, device=device)
+        ws, ws_bytes, held = _workspace("rollout_token_logprobs_workspace", device, rows, vocab, top)
+        logp, entropy = torch.empty(2, rows, device=device).unbind()
         stats = torch.empty(rows, 2, device=device)
         ids = torch.empty(rows, top, dtype=torch.int32, device=device) if top else None
         alt = torch.empty(rows, top, device=device) if top else None
         _enqueued(lib, lib.rollout_token_logprobs(
-            logits.data_ptr(), dtype, rows, vocab, stride, temperature, tgt, top, ws.data_ptr() if ws is not None else None,
-            len(ws) if ws is not None else 0, s, logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(),
+            logits.data_ptr(), dtype, rows, vocab, stride, temperature, tgt, top, ws, ws_bytes, s, logp.data_ptr(), entropy.data_ptr(), stats.data_ptr(),
             ids.data_ptr() if top else None, alt.data_ptr() if top else None))
     return logp, entropy, stats, ids, alt
 
@@ -656,10 +688,10 @@ def rollout_embed_grad(grad_rows, tokens, vocab, *, scale=1.0, base=None, dtype=
     with _On(device, stream) as s:
         if out is None:
             out = torch.empty(vocab, hidden, dtype=dtype, device=device)
-        ws = _workspace(lib, lib.rollout_embed_grad_workspace(n, vocab, hidden), device)
+        ws, ws_bytes, held = _workspace("rollout_embed_grad_workspace", device, n, vocab, hidden)
         _enqueued(lib, lib.rollout_embed_grad(grad_rows.data_ptr(), rows_dtype, n, vocab, hidden, stride, tok, scale,
                                               base.data_ptr() if base is not None else None, _dtype_id(out, "out"),
-                                              ws.data_ptr(), len(ws), s, out.data_ptr()))
+                                              ws, ws_bytes, s, out.data_ptr()))
     return out
 
 
@@ -684,11 +716,10 @@ def rollout_head_logprobs(hidden_states, lm_head, targets=None, *, temperature=1
     lib = load_library()
     device, rows, vocab, hidden, args, tgt = _head(hidden_states, lm_head, targets)
     with _On(device, stream) as s:
-        ws = _workspace(lib, lib.rollout_head_logprobs_workspace(rows, vocab, hidden), device)
-        logp, entropy = torch.empty(rows, device=device), torch.empty(rows, device=device)
+        ws, ws_bytes, held = _workspace("rollout_head_logprobs_workspace", device, rows, vocab, hidden)
+        logp, entropy = torch.empty(2, rows, device=device).unbind()
         stats = torch.empty(rows, 2, device=device)
-        _enqueued(lib, lib.rollout_head_logprobs(*args, temperature, tgt, ws.data_ptr() if ws is not None else None,
-                                                 len(ws) if ws is not None else 0, s, logp.data_ptr(), entropy.data_ptr(),
+        _enqueued(lib, lib.rollout_head_logprobs(*args, temperature, tgt, ws, ws_bytes, s, logp.data_ptr(), entropy.data_ptr(),
                                                  stats.data_ptr()))
     return logp, entropy, stats
 
@@ -706,11 +737,11 @@ def rollout_head_logprobs_grad(hidden_states, lm_head, targets, row_stats, entro
     gl = _vector(grad_logp, "grad_logp", device, torch.float32, rows)
     ge = _vector(grad_entropy, "grad_entropy", device, torch.float32, rows)
     with _On(device, stream) as s:
-        ws = _workspace(lib, lib.rollout_head_logprobs_grad_workspace(rows, vocab, hidden), device)
+        ws, ws_bytes, held = _workspace("rollout_head_logprobs_grad_workspace", device, rows, vocab, hidden)
         grad_hidden = torch.empty(rows, hidden, dtype=torch.bfloat16, device=device)
         grad_head = torch.empty(vocab, hidden, dtype=torch.bfloat16, device=device)
         _enqueued(lib, lib.rollout_head_logprobs_grad(*args, temperature, tgt, row_stats.data_ptr(), ent, gl, ge,
-                                                      ws.data_ptr(), len(ws), s, grad_hidden.data_ptr(),
+                                                      ws, ws_bytes, s, grad_hidden.data_ptr(),
                                                       grad_head.data_ptr()))
     return grad_hidden, grad_head
 

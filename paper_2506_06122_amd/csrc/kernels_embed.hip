@@ -4,7 +4,7 @@
 //
 // Both are bound by memory.  The gradient takes three launches.  The first sorts the rows by id and meanwhile writes
 // every row of the matrix (zeros, or the base), which is most of the bytes of a large vocabulary.  The second sums runs
-// of equal ids in fp32, in the order of the rows, so the result does not depend on scheduling.  It takes kChunk sorted
+// of equal ids in fp32, in the order of the rows, so the result does not depend on scheduling.  It takes a chunk of sorted
 // rows to a workgroup whatever the ids are: a run that crosses the edge of a chunk leaves partial sums, and the third
 // launch joins those in order.
 #include "vocab.h"
@@ -58,7 +58,9 @@ void launch_rows(const EmbedArgs& a, hipStream_t s) {
 // ---- gradient ------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / WAVE;
 constexpr int kRange = 512;   // ids of a sorting workgroup at most: kSortWaves counters each are 32 KB of LDS
-constexpr int kChunk = 16;    // sorted rows of a summing workgroup
+// sorted rows of a summing workgroup: as many rows as fill the card, each workgroup with a few in flight; with many rows more,
+// since each chunk may leave two rows of partial sums
+constexpr int chunk_rows(int n) { return n <= 4096 ? 4 : 16; }
 constexpr int kFill = 8192;   // 16-byte vectors of the matrix that a filling workgroup writes
 
 struct EmbedSort {
@@ -70,7 +72,7 @@ struct EmbedSort {
 };
 struct EmbedPlan {
   int ranges, range;  // sorting workgroups and the ids of each
-  int chunks;
+  int chunk, chunks;
 };
 EmbedPlan plan(int n, int vocab) {
   EmbedPlan p;
@@ -78,7 +80,8 @@ EmbedPlan plan(int n, int vocab) {
   const int wanted = std::max(ceil_div(vocab, kRange), std::min(256, ceil_div(n, 16)));
   p.range = ceil_div(vocab, std::min(wanted, vocab));
   p.ranges = ceil_div(vocab, p.range);
-  p.chunks = ceil_div(n, kChunk);
+  p.chunk = chunk_rows(n);
+  p.chunks = ceil_div(n, p.chunk);
   return p;
 }
 
@@ -209,7 +212,7 @@ __device__ inline void store_row(const EmbedGrad& a, int id, int col, const floa
   }
 }
 
-template <typename V, typename G, bool VEC>
+template <typename V, typename G, bool VEC, int kChunk>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGrad a, EmbedSort q) {
   constexpr int E = VEC ? 8 : 1;
   __shared__ int row_s[kChunk], id_s[kChunk + 2];  // ids from the one before the chunk to the one behind it
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGrad a, EmbedSort q
 
 // A run that leaves its chunk: the chunk in which it begins takes the shares of the following ones, in order.
 template <typename G, bool VEC>
-__global__ __launch_bounds__(64) void embed_join_kernel(EmbedGrad a, EmbedSort q) {
+__global__ __launch_bounds__(64) void embed_join_kernel(EmbedGrad a, EmbedSort q, int kChunk) {
   constexpr int E = VEC ? 8 : 1;
   const int chunk = blockIdx.x, col = (blockIdx.y * 64 + threadIdx.x) * E;
   const int n = *q.n_inside, next = (chunk + 1) * kChunk;
@@ -318,11 +321,11 @@ void launch_grad(const EmbedGrad& a, void* ws, hipStream_t s) {
   const bool vec = a.hidden % 8 == 0 && a.row_stride % 8 == 0 && (((size_t)a.grad_rows | (size_t)a.base | (size_t)a.out) & 15) == 0;
   const int cols = vec ? a.hidden / 8 : a.hidden, threads = std::min(256, ceil_div(cols, 64) * 64);
   const dim3 grid(p.chunks, ceil_div(cols, threads)), join(p.chunks - 1, ceil_div(cols, 64));
-  if (vec) embed_sum_kernel<V, G, true><<<grid, threads, 0, s>>>(a, q);
-  else embed_sum_kernel<V, G, false><<<grid, threads, 0, s>>>(a, q);
+  if (vec) p.chunk == 4 ? embed_sum_kernel<V, G, true, 4><<<grid, threads, 0, s>>>(a, q) : embed_sum_kernel<V, G, true, 16><<<grid, threads, 0, s>>>(a, q);
+  else p.chunk == 4 ? embed_sum_kernel<V, G, false, 4><<<grid, threads, 0, s>>>(a, q) : embed_sum_kernel<V, G, false, 16><<<grid, threads, 0, s>>>(a, q);
   if (p.chunks == 1) return;
-  if (vec) embed_join_kernel<G, true><<<join, 64, 0, s>>>(a, q);
-  else embed_join_kernel<G, false><<<join, 64, 0, s>>>(a, q);
+  if (vec) embed_join_kernel<G, true><<<join, 64, 0, s>>>(a, q, p.chunk);
+  else embed_join_kernel<G, false><<<join, 64, 0, s>>>(a, q, p.chunk);
 }
 
 }  // namespace

@@ -276,6 +276,17 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
   const bool has_target = target >= 0 && target < in.vocab;
   const float x_target = has_target ? to_f32(((const V*)in.logits + r * in.stride)[target]) : 0.f;
   if (tid == 0) n_s = 0;
+  // what is looked at later is on its way meanwhile: the first keys of every thread, and of every part's `deep` greatest the
+  // last (see below)
+  constexpr int AHEAD = 5;
+  const unsigned long long* keys = p.keys + (long long)r * p.parts * out.top;
+  const int n_keys = p.parts * out.top, deep = (2 * out.top + p.parts - 1) / p.parts, wide = TOP ? (out.top + deep - 1) / deep : 0;
+  unsigned long long ahead[AHEAD], deep_key = 0;
+  if constexpr (TOP) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) ahead[u] = tid + u * T < n_keys ? keys[tid + u * T] : 0;
+    if (tid < p.parts) deep_key = keys[(long long)tid * out.top + deep - 1];
+  }
   RowSums mine{kLowest, 0.f, 0.f};
   for (int i = tid; i < p.parts; i += T) mine = merge(mine, p.sums[(long long)r * p.parts + i], c);
   mine = merge_wave(mine, c);
@@ -288,10 +299,8 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
   if constexpr (TOP) {
     // Of every part's `deep` greatest keys the last: the `wide`-th greatest of these is a bound that K keys reach, and
     // with about half the parts above it few more do
-    const unsigned long long* keys = p.keys + (long long)r * p.parts * out.top;
-    const int deep = (2 * out.top + p.parts - 1) / p.parts, wide = (out.top + deep - 1) / deep;
     if (wave == 0) {
-      const unsigned long long key = lane < p.parts ? keys[(long long)lane * out.top + deep - 1] : 0;
+      const unsigned long long key = deep_key;
       int rank = 0;
       for (int j = 0; j < p.parts; ++j) {
         const unsigned long long other = (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 |
@@ -302,7 +311,10 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
     }
     __syncthreads();
     const unsigned long long least = max(least_s, 1ull);
-    for (int i = tid; i < p.parts * out.top; i += T) {
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (ahead[u] >= least) listed[atomicAdd(&n_s, 1)] = ahead[u];
+    for (int i = tid + AHEAD * T; i < n_keys; i += T) {
       const unsigned long long key = keys[i];
       if (key >= least) listed[atomicAdd(&n_s, 1)] = key;
     }
