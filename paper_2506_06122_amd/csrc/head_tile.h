@@ -21,13 +21,13 @@ struct HeadSlice {
   static constexpr int swizzle(int k) { return 2 * ((k & 3) + 4 * (k >> 3 & 1)) & (chunks - 1); }
   // byte offset in memory, from the slice's first value, of lane's 16 bytes of unit u; rows (columns) past `limit` and
   // steps past k_left read the last one
-  static constexpr long long source(int u, int lane, int limit, int k_left, long long op_pitch) {
+  static constexpr unsigned source(int u, int lane, int limit, int k_left, int op_pitch) {
     if (KM) {
       const int at = u * 1024 + lane * 16, k = at / pitch, slot = at % pitch / 16, col = (slot ^ swizzle(k)) * 8;
-      return (head_min(k, k_left - 1) * op_pitch + head_min(col, limit - 8)) * 2;
+      return ((unsigned)head_min(k, k_left - 1) * (unsigned)op_pitch + (unsigned)head_min(col, limit - 8)) * 2;
     }
     const int row = u * 8 + (lane >> 3), chunk = (lane & 7) ^ (row & 7);
-    return (head_min(row, limit - 1) * op_pitch + chunk * 8) * 2;
+    return ((unsigned)head_min(row, limit - 1) * (unsigned)op_pitch + chunk * 8) * 2;
   }
   // LDS byte of a lane's part of the fragment of columns 16 i .., steps 32 half ..: lane = 16 g + r.  Rows outermost: the
   // 16 bytes of column r, steps 8 g ...  K outermost: 8 bytes of step 8 g + r / 4, columns 4 (r % 4) ..., and again four
@@ -178,8 +178,17 @@ constexpr HeadMost head_most(const HeadGradPlan& g, int rows, int vocab, int hid
   }
   return most;
 }
-// columns between the rows of a chunk's gradients: the padding of K in the product that follows, and of its tiles
-constexpr int head_grad_pitch(int columns) { return head_up(columns, 256); }
+// The gradients of logits lie in panels of 256 columns, row below row, so that both products that read them find a slice
+// together: 64 rows of 512 bytes one behind the other, or 256 rows 512 bytes apart, where rows of a vocabulary's length
+// put every one on a page of its own.
+constexpr int kHeadPanel = 256;
+constexpr long long head_panel_at(int row, int col, int room) {
+  return ((long long)(col / kHeadPanel) * room + row) * kHeadPanel + col % kHeadPanel;
+}
+// The slice kt of a panelled operand, from its first row (rows outermost) or column (K outermost)
+constexpr long long head_panel_slice(bool km, int first, int kt, int room) {
+  return km ? head_panel_at(kt * kHeadDeep, first, room) : head_panel_at(first, kt * kHeadDeep, room);
+}
 
 // One tile's share of a product, with the sizes that only the device knows filled in.
 struct HeadExtent {
@@ -189,15 +198,14 @@ struct HeadExtent {
   int b_last;            // steps of B's last slice that exist
 };
 constexpr HeadExtent head_extent(bool a_km, bool b_km, bool pad_rows, int m0, int n0, int z, int M, int N, int K, int per_split,
-                                 long long a_pitch, int row_capacity) {
+                                 int row_capacity) {
   HeadExtent x{};
   x.m_end = pad_rows ? head_min(row_capacity, head_up(M, kHeadDeep)) : M;
   x.k_tiles = head_ceil(K, kHeadDeep);
   x.kt_begin = z * per_split;
   x.kt_end = head_min(x.k_tiles, x.kt_begin + per_split);
-  // (with K outermost a row of A ends at its pitch, past the last column that is stored; with rows outermost the padding
-  // rows exist too, as zeros)
-  x.a_limit = (a_km ? (int)a_pitch : x.m_end) - m0;
+  // (A with K outermost is panelled, whole tiles; with rows outermost the padding rows exist too, as zeros)
+  x.a_limit = a_km ? kHeadPanel - m0 % kHeadPanel : x.m_end - m0;
   x.b_limit = N - n0;
   x.b_last = b_km ? K - (x.k_tiles - 1) * kHeadDeep : kHeadDeep;
   return x;

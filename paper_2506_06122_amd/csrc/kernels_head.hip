@@ -30,7 +30,7 @@ enum { TO_SUMS, TO_GRAD, TO_PLANE, TO_BF16 };
 
 struct Operand {
   const void* p;
-  long long pitch;  // elements between rows, or with the summed index outermost between its steps
+  int pitch;  // elements between rows, or with the summed index outermost between its steps
 };
 struct Product {
   Operand a, b;
@@ -39,6 +39,7 @@ struct Product {
   HeadGrid grid;
   void* out;
   long long out_pitch;
+  int room;               // rows of the panels that the gradients of logits lie in: TO_GRAD's result, the next products' A
   bool add;
   float inv_temp;
   // TO_SUMS
@@ -59,6 +60,19 @@ __device__ __forceinline__ void load_to_lds(unsigned lds, unsigned voff, const v
 template <int N>
 __device__ __forceinline__ void wait_and_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+// over the four lanes that hold a row's columns, 16 and 32 lanes apart, in each of them
+__device__ __forceinline__ float column_max(float x) {
+  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+  const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ __forceinline__ float column_sum(float x) {
+  const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+  const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 template <class F, int... I>
 __device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>) {
@@ -112,7 +126,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
   const int bn = block.n, bz = block.z;
   const int m0 = block.m * BM, n0 = bn * BN;
   const HeadExtent x = head_extent(AK, BK, TO == TO_GRAD, m0, n0, bz, M, p.N, K, TO == TO_PLANE ? head_ceil(head_ceil(K, kHeadDeep), grid.splits) : head_ceil(K, kHeadDeep),
-                                   p.a.pitch, p.row_capacity);
+                                   p.row_capacity);
   if (m0 >= x.m_end) return;
   const int k_tiles = x.k_tiles, kt_begin = x.kt_begin, kt_end = x.kt_end;
 
@@ -126,19 +140,24 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
     // this wavefront's loads of a stage: units wave, wave + NW, ... of A's, then B's; their sources move on with the slices
     unsigned voff[L], tail[L], dst[L];
     bool is_b[L];
-    const long long a_step = (AK ? p.a.pitch : 1) * 2 * kHeadDeep, b_step = (BK ? p.b.pitch : 1) * 2 * kHeadDeep;
-    const char* pa = (const char*)p.a.p + 2 * (AK ? m0 : m0 * p.a.pitch) + kt_begin * a_step;
-    const char* pb = (const char*)p.b.p + 2 * (BK ? n0 : n0 * p.b.pitch) + kt_begin * b_step;
+    constexpr bool PANELS = TO == TO_PLANE || TO == TO_BF16;
+    const int a_pitch = PANELS ? kHeadPanel : p.a.pitch;
+    const long long b_step = (BK ? (long long)p.b.pitch : 1) * 2 * kHeadDeep;
+    const auto a_slice = [&](int kt) __attribute__((always_inline)) {
+      return (const char*)p.a.p + 2 * (PANELS ? head_panel_slice(AK, m0, kt, p.room) : (long long)m0 * p.a.pitch + kt * kHeadDeep);
+    };
+    const char* pa = a_slice(kt_begin);
+    const char* pb = (const char*)p.b.p + 2 * (BK ? n0 : (long long)n0 * p.b.pitch) + kt_begin * b_step;
 #pragma unroll
     for (int s = 0; s < L; ++s) {
       const int u = __builtin_amdgcn_readfirstlane(min(s * NW + wave, U - 1));  // an uneven last round loads the last one again
       is_b[s] = u >= A::units;
       dst[s] = u * 1024;
       if (!is_b[s]) {
-        tail[s] = voff[s] = (unsigned)A::source(u, lane, x.a_limit, kHeadDeep, p.a.pitch);
+        tail[s] = voff[s] = A::source(u, lane, x.a_limit, kHeadDeep, a_pitch);
       } else {
-        voff[s] = (unsigned)B::source(u - A::units, lane, x.b_limit, kHeadDeep, p.b.pitch);
-        tail[s] = BK ? (unsigned)B::source(u - A::units, lane, x.b_limit, x.b_last, p.b.pitch) : voff[s];
+        voff[s] = B::source(u - A::units, lane, x.b_limit, kHeadDeep, p.b.pitch);
+        tail[s] = BK ? B::source(u - A::units, lane, x.b_limit, x.b_last, p.b.pitch) : voff[s];
       }
     }
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) void*)lds;
@@ -151,7 +170,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
     auto move_on = [&]() __attribute__((always_inline)) {
       if (ahead + 1 < kt_end) {
         ++ahead;
-        pa += a_step;
+        pa = a_slice(ahead);
         pb += b_step;
       }
     };
@@ -245,10 +264,12 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[4 * j + e] = whole || col + j * 16 + e < p.N ? acc[i][j][e] : -INFINITY;
-      RowSums s{kLowest, 0.f, 0.f};
-      add_chunk<4 * NT>(s, v, c);
+      float top = v[0];
 #pragma unroll
-      for (int o = 16; o < 64; o <<= 1) s = merge(s, RowSums{__shfl_xor(s.m, o, WAVE), __shfl_xor(s.s, o, WAVE), __shfl_xor(s.t, o, WAVE)}, c);
+      for (int k = 1; k < 4 * NT; ++k) top = fmaxf(top, v[k]);
+      RowSums s = sum_below<4 * NT>(column_max(fmaxf(top, kLowest)), 0.f, 0.f, v, c);
+      s.s = column_sum(s.s);
+      s.t = column_sum(s.t);
       if (g == 0) part[wn * BM + ml] = s;
     }
     __syncthreads();
@@ -314,8 +335,9 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
     }
     // columns that exist: the product's, or as far as the padding of K in the product that follows
     constexpr int LANES = NT * 2, ROWS = 64 / LANES;  // lanes to a row, rows at a time
-    const int n = col0 + lane % LANES * 8, n_end = TO == TO_GRAD ? (int)p.out_pitch : p.N;
-    uint16_t* out = (uint16_t*)p.out;
+    const int n = col0 + lane % LANES * 8, n_end = TO == TO_GRAD ? head_up(p.N, kHeadPanel) : p.N;
+    const long long out_pitch = TO == TO_GRAD ? kHeadPanel : p.out_pitch;
+    uint16_t* out = (uint16_t*)p.out + (TO == TO_GRAD ? head_panel_at(0, n, p.room) : n);
     constexpr bool TWO = TO == TO_GRAD && BM <= 128;  // tiles of few rows
 #pragma unroll 1
     for (int plane = 0; plane < (TWO ? p.planes : 1); ++plane) {
@@ -335,9 +357,9 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
       for (int q = 0; q < MT * 16; q += ROWS) {
         const int ml = q + lane / LANES, m = m0 + wm * MT * 16 + ml;
         const u32x4 w = *(const u32x4*)(mine + ml * OUT_ROW + lane % LANES * 16);
-        if (m < x.m_end && n < n_end) *(u32x4*)(out + m * p.out_pitch + n) = w;
+        if (m < x.m_end && n < n_end) *(u32x4*)(out + m * out_pitch) = w;
       }
-      out += head_up(M, kHeadDeep) * p.out_pitch;
+      out += head_up(M, kHeadDeep) * out_pitch;
     }
   }
 }
@@ -456,8 +478,8 @@ size_t head_workspace(int rows, int vocab, int) {
 void launch_head_logprobs(const HeadArgs& in, const TokenOut& out, void* ws, hipStream_t s) {
   const HeadTile t = head_tile(in.rows, in.vocab);
   Product p{};
-  p.a = {in.hidden_states, in.hidden_stride};
-  p.b = {in.lm_head, in.head_stride};
+  p.a = {in.hidden_states, (int)in.hidden_stride};
+  p.b = {in.lm_head, (int)in.head_stride};
   p.M = in.rows;
   p.N = in.vocab;
   p.K = in.hidden;
@@ -500,13 +522,13 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
     if (in.rows > 0) {
       Product p{};  // logits of the chunk and their gradients
       p.a = {h, in.hidden};
-      p.b = {w, in.head_stride};
+      p.b = {w, (int)in.head_stride};
       p.M = in.rows;
       p.N = v;
       p.K = in.hidden;
       p.plan = plan;
       p.out = dx;
-      p.out_pitch = head_grad_pitch(v);
+      p.room = (int)room;
       p.inv_temp = in.inv_temp;
       p.targets = in.targets;
       p.active = active;
@@ -520,8 +542,9 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
       p.planes = g.planes;
       launch_product<TO_GRAD, false, false>(p, head_tile_logits(in.rows, v), 0, s);
       Product q{};  // + dx W
-      q.a = {dx, p.out_pitch};
-      q.b = {w, in.head_stride};
+      q.a = {dx, kHeadPanel};
+      q.room = (int)room;
+      q.b = {w, (int)in.head_stride};
       q.M = (int)room;
       q.N = in.hidden;
       q.K = v;
@@ -532,7 +555,8 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
       launch_product<TO_PLANE, false, true>(q, head_tile_hidden((int)room), most.blocks, s);
     }
     Product q{};  // dx^T h
-    q.a = {dx, head_grad_pitch(v)};
+    q.a = {dx, kHeadPanel};
+    q.room = (int)room;
     q.b = {h, in.hidden};
     q.M = v;
     q.N = in.hidden;

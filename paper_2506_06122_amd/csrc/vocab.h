@@ -92,16 +92,11 @@ __device__ inline RowSums merge(const RowSums& p, const RowSums& q, float c) {
   const float fp = __builtin_amdgcn_exp2f(-dp), fq = __builtin_amdgcn_exp2f(-dq);
   return RowSums{m, p.s * fp + q.s * fq, (p.t - dp * p.s) * fp + (q.t - dq * q.s) * fq};
 }
-// N more values; returns their maximum.  The quick form makes a NaN of 0 x -inf for values of -inf (and of anything the plain exponent
-// cannot hold): such chunks are summed again with care, and what is NaN or +inf among the values stays NaN.
+// s and t with N more values, none above m.  The quick form makes a NaN of 0 x -inf for values of -inf (and of anything the
+// plain exponent cannot hold): such chunks are summed again with care, and what is NaN or +inf among the values stays NaN.
 template <int N>
-__device__ inline float add_chunk(RowSums& r, const float* v, float c) {
-  float top = v[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
-  const float m = fmaxf(r.m, top);
-  const float d = raise(r.m, m, c), f = __builtin_amdgcn_exp2f(-d), ref = rintf(m * c);
-  const float t0 = (r.t - d * r.s) * f, s0 = r.s * f;
+__device__ inline RowSums sum_below(float m, float s0, float t0, const float* v, float c) {
+  const float ref = rintf(m * c);
   float s = s0, t = t0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -120,7 +115,16 @@ __device__ inline float add_chunk(RowSums& r, const float* v, float c) {
       t = fmaf(e, fmaxf(y, -1e30f), t);
     }
   }
-  r = RowSums{m, s, t};
+  return RowSums{m, s, t};
+}
+// N more values; returns their maximum
+template <int N>
+__device__ inline float add_chunk(RowSums& r, const float* v, float c) {
+  float top = v[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
+  const float m = fmaxf(r.m, top), d = raise(r.m, m, c), f = __builtin_amdgcn_exp2f(-d);
+  r = sum_below<N>(m, r.s * f, (r.t - d * r.s) * f, v, c);
   return top;
 }
 

@@ -25,6 +25,8 @@ struct Product {
   long long a_pitch, b_pitch, out_pitch, out_size;
   int m_room, M, N, K, capacity, splits, blocks;  // M, K, splits: as the device finds them
   long long out_row;                              // rows before the first one's
+  bool panels;                                    // A is panelled; with pad_rows the result is
+  int room;
 };
 
 template <int C, bool KM>
@@ -32,7 +34,7 @@ static void loads(const char* name, long long base, int limit, int k_left, long 
   using S = HeadSlice<C, KM>;
   for (int u = 0; u < S::units; ++u)
     for (int lane = 0; lane < 64; ++lane) {
-      const long long off = S::source(u, lane, limit, k_left, pitch), at = base + off;
+      const long long off = S::source(u, lane, limit, k_left, (int)pitch), at = base + off;
       if (off < 0 || off >= 1ll << 32) bad("offset does not fit", name, u, lane, limit, off);
       if (at < 0 || at + 16 > arr.bytes) bad("load out of range", name, u, lane, at, arr.bytes);
       if (at % 16) bad("load not aligned", name, u, lane, at, 0);
@@ -66,20 +68,21 @@ static void walk(const Product& p) {
     for (int n : ns)
       for (int z : zs) {
         const int m0 = m * BM, n0 = n * BN;
-        const HeadExtent x = head_extent(AK, BK, p.pad_rows, m0, n0, z, M, p.N, K, per, p.a_pitch, p.capacity);
+        const HeadExtent x = head_extent(AK, BK, p.pad_rows, m0, n0, z, M, p.N, K, per, p.capacity);
         if (m0 >= x.m_end) continue;
         std::set<int> kts;
         if (x.kt_begin < x.kt_end && m0 < M) kts = {x.kt_begin, x.kt_end - 1, (x.kt_begin + x.kt_end) / 2};
         for (int kt : kts) {
-          const long long a0 = 2 * (AK ? m0 + kt * kHeadDeep * p.a_pitch : m0 * p.a_pitch + kt * kHeadDeep), b0 = 2 * (BK ? n0 + kt * kHeadDeep * p.b_pitch : n0 * p.b_pitch + kt * kHeadDeep);
+          const long long a0 = 2 * (p.panels ? head_panel_slice(AK, m0, kt, p.room) : m0 * p.a_pitch + kt * kHeadDeep), b0 = 2 * (BK ? n0 + kt * kHeadDeep * p.b_pitch : n0 * p.b_pitch + kt * kHeadDeep);
           loads<BM, AK>(p.name, a0, x.a_limit, kHeadDeep, p.a_pitch, p.a);
           loads<BN, BK>(p.name, b0, x.b_limit, BK && kt == x.k_tiles - 1 ? x.b_last : kHeadDeep, p.b_pitch, p.b);
         }
         // stores of four values: last row of the tile, last column that passes the kernel's test
         const int row = head_min(m0 + BM, x.m_end) - 1;
-        const int cols = p.pad_rows ? (int)p.out_pitch : p.N, col = head_min(n0 + BN, cols) - 4;
-        const long long at = ((p.splits > 1 ? (long long)z * M + row : p.out_row + row) * p.out_pitch + col) * p.out_size;
-        if (p.out.bytes && (at < 0 || at + 4 * p.out_size > p.out.bytes)) bad("store out of range", p.name, row, col, at, p.out.bytes);
+        const int cols = p.pad_rows ? head_up(p.N, kHeadPanel) : p.N, col = head_min(n0 + BN, cols) - 8;
+        const long long at = (p.pad_rows ? head_panel_at((int)p.out_row + row, col, p.room)
+                                         : (p.splits > 1 ? (long long)z * M + row : p.out_row + row) * p.out_pitch + col) * p.out_size;
+        if (p.out.bytes && (at < 0 || at + 8 * p.out_size > p.out.bytes)) bad("store out of range", p.name, row, col, at, p.out.bytes);
         ++checks;
       }
 }
@@ -97,7 +100,7 @@ static void by_tile(const Product& p) {
 static void sizes(int rows, int vocab, int hidden, int pad) {
   const long long hp = hidden + pad;
   const Array states{(rows - 1) * hp * 2 + hidden * 2}, head{(vocab - 1) * hp * 2 + hidden * 2ll};
-  by_tile<false, false>({"logits", head_tile(rows, vocab), false, states, head, {0}, hp, hp, 0, 0, rows, rows, vocab, hidden, 0, 1, 0, 0});
+  by_tile<false, false>({"logits", head_tile(rows, vocab), false, states, head, {0}, hp, hp, 0, 0, rows, rows, vocab, hidden, 0, 1, 0, 0, false, 0});
   const HeadGradPlan g = head_grad_plan(rows, vocab);
   const HeadMost most = head_most(g, rows, vocab, hidden);
   const int room = g.rows * g.planes;
@@ -109,14 +112,13 @@ static void sizes(int rows, int vocab, int hidden, int pad) {
     const HeadActive a = head_active(count, g, vocab, hidden);
     if (a.stacked > room || a.splits < 1) bad("plan", "active", count, a.stacked, room, a.splits);
     for (int v0 = 0; v0 < vocab; v0 += g.chunk) {
-      const int v = head_min(g.chunk, vocab - v0), pitch = head_grad_pitch(v);
-      if (pitch > g.chunk || pitch % 256 || pitch < v) bad("pitch", "gradients", pitch, g.chunk, v, 0);
+      const int v = head_min(g.chunk, vocab - v0);
       const Array w{(long long)(v - 1) * hp * 2 + hidden * 2ll + (long long)(vocab - v0 - v) * hp * 2};
       for (int plane = 0; plane < g.planes; ++plane)
-        by_tile<false, false>({"gradients", head_tile_logits(rows, v), true, h, w, dx, hidden, hp, pitch, 2, rows, count, v, hidden, g.rows, 1, 0,
-                               (long long)plane * head_up(count, kHeadDeep)});
-      by_tile<false, true>({"grad_hidden", head_tile_hidden(room), false, dx, w, parts, pitch, hp, hidden, 4, room, a.stacked, hidden, v, 0, a.splits, most.blocks, 0});
-      by_tile<true, true>({"grad_head", head_tile_head(rows), false, dx, h, {(long long)v * hidden * 2}, pitch, hidden, hidden, 2, v, v, hidden, a.stacked, 0, 1, 0, 0});
+        by_tile<false, false>({"gradients", head_tile_logits(rows, v), true, h, w, dx, hidden, hp, 0, 2, rows, count, v, hidden, g.rows, 1, 0,
+                               (long long)plane * head_up(count, kHeadDeep), false, room});
+      by_tile<false, true>({"grad_hidden", head_tile_hidden(room), false, dx, w, parts, kHeadPanel, hp, hidden, 4, room, a.stacked, hidden, v, 0, a.splits, most.blocks, 0, true, room});
+      by_tile<true, true>({"grad_head", head_tile_head(rows), false, dx, h, {(long long)v * hidden * 2}, kHeadPanel, hidden, hidden, 2, v, v, hidden, a.stacked, 0, 1, 0, 0, true, room});
     }
   }
 }
