@@ -388,14 +388,15 @@ int rollout_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int3
  * row_stats and entropy as rollout_token_logprobs left them for the same logits, temperature and targets; grad_entropy
  * may be NULL, entropy then too.  grad_logp of a row without a target counts for nothing.  A row whose gradients are
  * both 0, and a row of -inf alone, gets zeros, its logits unread.  grad_logits has the logits' dtype and may be the
- * logits array itself with the same row stride; otherwise the two must not overlap.  What lies between the rows is left as it was. */
+ * logits array itself with the same row stride; otherwise the two must not overlap (rows of one stride may lie between
+ * each other's).  What lies between the rows is left as it was. */
 int rollout_token_logprobs_grad(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,
                                 float temperature, const int32_t *targets, const float *row_stats, const float *entropy,
                                 const float *grad_logp, const float *grad_entropy, void *hip_stream, void *grad_logits,
                                 int64_t grad_row_stride);
 
 /* out[r] = scale * table[tokens[r]], rounded once to dtype; zeros for ids outside [0, vocab) (padding).
- * table [vocab][hidden], out [n][hidden] without gaps. */
+ * table [vocab][hidden], out [n][hidden] without gaps, apart from the table. */
 int rollout_embed(const void *table, int32_t dtype, int32_t vocab, int32_t hidden, int64_t table_stride,
                   const int32_t *tokens, int32_t n, float scale, void *hip_stream, void *out);
 
@@ -403,7 +404,7 @@ int rollout_embed(const void *table, int32_t dtype, int32_t vocab, int32_t hidde
  * in the order of r, fp32, rounded once to table_dtype (dtype or ROLLOUT_DTYPE_F32).  Ids outside [0, vocab) add nothing.
  * base [vocab][hidden] of table_dtype, or NULL (0): a tied matrix takes the gradient of the lm_head here.  base may be
  * grad_table itself - then rows of ids that do not occur are neither read nor written - and must not overlap it
- * otherwise.  grad_rows [n][hidden] of dtype; grad_table and base without gaps. */
+ * otherwise.  grad_rows [n][hidden] of dtype, apart from grad_table; grad_table and base without gaps. */
 int64_t rollout_embed_grad_workspace(int32_t n, int32_t vocab, int32_t hidden);
 int rollout_embed_grad(const void *grad_rows, int32_t dtype, int32_t n, int32_t vocab, int32_t hidden, int64_t row_stride,
                        const int32_t *tokens, float scale, const void *base, int32_t table_dtype, void *workspace,
@@ -420,7 +421,9 @@ int rollout_head_logprobs(const void *hidden_states, int64_t hidden_stride, cons
 
 /* Its gradients with respect to hidden_states and lm_head, from the logits' gradient g as in rollout_token_logprobs_grad
  * (rounded to bf16 for the products): grad_hidden = g . lm_head [rows][hidden], grad_head = g^T . hidden_states
- * [vocab][hidden], both bf16 without gaps.  Rows whose gradients are both 0 take no part: their grad_hidden is 0. */
+ * [vocab][hidden], both bf16 without gaps, apart from each other and from the inputs.  Rows whose gradients are both 0
+ * take no part: their grad_hidden is 0.  With at most 128 rows g is kept as a bf16 value and the bf16 rest: one rounding
+ * of a row's largest gradient would show in both results; over more rows that averages out. */
 int64_t rollout_head_logprobs_grad_workspace(int32_t rows, int32_t vocab, int32_t hidden);
 int rollout_head_logprobs_grad(const void *hidden_states, int64_t hidden_stride, const void *lm_head, int64_t head_stride,
                                int32_t rows, int32_t vocab, int32_t hidden, float temperature, const int32_t *targets,

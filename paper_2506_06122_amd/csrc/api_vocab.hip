@@ -17,6 +17,14 @@ void check_sizes(int rows, int vocab, int hidden) {
   if (vocab < 1 || vocab > kMaxVocab) fail(ROLLOUT_E_INVAL, "vocab must be within 1 .. 2^24");
   if (hidden < 1 || hidden > kMaxHidden) fail(ROLLOUT_E_INVAL, "hidden must be within 1 .. 2^20");
 }
+// what the launches count in 32 bits
+void check_product(int rows, int hidden) {
+  if ((int64_t)rows * hidden > (int64_t)1 << 38) fail(ROLLOUT_E_INVAL, "rows x hidden must not exceed 2^38");
+}
+void check_tiles(int rows, int vocab) {
+  if ((int64_t)(rows / 128 + 1) * (vocab / 128 + 1) > (int64_t)1 << 28)
+    fail(ROLLOUT_E_INVAL, "rows x vocab must not exceed 2^42");
+}
 void check_dtype(int dtype) {
   if (dtype != VT_F32 && dtype != VT_BF16 && dtype != VT_F16) fail(ROLLOUT_E_INVAL, "unknown dtype");
 }
@@ -51,6 +59,24 @@ void check_workspace(const void* p, size_t bytes, size_t need) {
     fail(ROLLOUT_E_INVAL, "workspace of " + std::to_string(bytes) + " bytes, " + std::to_string(need) + " are needed");
   check_array(p, 16, "workspace");
 }
+// Two arrays of `rows` rows each, in bytes, that must not share any: rows of one stride may lie between each other's.
+struct Extent {
+  size_t at;
+  int64_t rows, width, stride;
+  size_t end() const { return at + (size_t)((rows - 1) * stride + width); }
+};
+Extent extent(const void* p, int64_t rows, int64_t width, int64_t stride, size_t size) {
+  return Extent{(size_t)p, rows, width * (int64_t)size, stride * (int64_t)size};
+}
+void check_apart(const Extent& a, const Extent& b, const char* names) {
+  if (a.rows <= 0 || b.rows <= 0 || a.end() <= b.at || b.end() <= a.at) return;
+  if (a.stride == b.stride && a.rows > 1 && b.rows > 1) {
+    const int64_t d = (int64_t)((b.at > a.at ? b.at - a.at : a.at - b.at) % (size_t)a.stride);
+    const int64_t first = b.at > a.at ? a.width : b.width, second = b.at > a.at ? b.width : a.width;
+    if (d >= first && d + second <= a.stride) return;
+  }
+  fail(ROLLOUT_E_INVAL, std::string(names) + " must not overlap");
+}
 void check_top(int top, int vocab) {
   if (top < 0 || top > ROLLOUT_TOP_MAX || top > vocab) fail(ROLLOUT_E_INVAL, "top must be within 0 .. min(vocab, ROLLOUT_TOP_MAX)");
 }
@@ -81,6 +107,8 @@ HeadArgs head_args(const void* hidden_states, int64_t hidden_stride, const void*
                    int vocab, int hidden, float temperature, const int32_t* targets) {
   check_sizes(rows, vocab, hidden);
   if (hidden % 64) fail(ROLLOUT_E_INVAL, "hidden must be a multiple of 64");
+  check_product(rows, hidden);
+  check_tiles(rows, vocab);
   check_operand_stride(hidden_stride, hidden, "hidden_stride");
   check_operand_stride(head_stride, hidden, "head_stride");
   check_optional(targets, 4, "targets");
@@ -143,7 +171,10 @@ int rollout_token_logprobs_grad(const void* logits, int32_t dtype, int32_t rows,
     check_array(grad_logits, vt_size(dtype), "grad_logits");
     check_optional(targets, 4, "targets");
     check_gradients(row_stats, entropy, grad_logp, grad_entropy);
-    if (grad_logits == logits && grad_row_stride != row_stride)
+    if (grad_logits != logits)
+      check_apart(extent(logits, rows, vocab, row_stride, vt_size(dtype)),
+                  extent(grad_logits, rows, vocab, grad_row_stride, vt_size(dtype)), "logits and grad_logits");
+    else if (grad_row_stride != row_stride)
       fail(ROLLOUT_E_INVAL, "gradients in place of the logits need their row stride");
     const TokenGrad a{{logits, row_stride, dtype, rows, vocab, inv_temp, targets}, row_stats, entropy, grad_logp,
                       grad_entropy, grad_logits, grad_row_stride};
@@ -162,6 +193,9 @@ int rollout_embed(const void* table, int32_t dtype, int32_t vocab, int32_t hidde
     check_array(table, vt_size(dtype), "table");
     check_array(tokens, 4, "tokens");
     check_array(out, vt_size(dtype), "out");
+    check_product(n, hidden);
+    check_apart(extent(table, vocab, hidden, table_stride, vt_size(dtype)), extent(out, n, hidden, hidden, vt_size(dtype)),
+                "table and out");
     const EmbedArgs a{table, table_stride, dtype, vocab, hidden, tokens, n, scale, out};
     enqueue([&] { launch_embed_rows(a, (hipStream_t)hip_stream); });
   });
@@ -189,6 +223,9 @@ int rollout_embed_grad(const void* grad_rows, int32_t dtype, int32_t n, int32_t 
     }
     check_optional(base, vt_size(table_dtype), "base");
     check_array(grad_table, vt_size(table_dtype), "grad_table");
+    const Extent result = extent(grad_table, vocab, hidden, hidden, vt_size(table_dtype));
+    check_apart(extent(grad_rows, n, hidden, row_stride, vt_size(dtype)), result, "grad_rows and grad_table");
+    if (base && base != grad_table) check_apart(extent(base, vocab, hidden, hidden, vt_size(table_dtype)), result, "base and grad_table");
     check_workspace(workspace, workspace_bytes, embed_grad_workspace(n, vocab, hidden));
     const EmbedGrad a{grad_rows, row_stride, dtype, tokens, n, vocab, hidden, scale, base, table_dtype, grad_table};
     enqueue([&] { launch_embed_grad(a, workspace, (hipStream_t)hip_stream); });
@@ -198,6 +235,8 @@ int rollout_embed_grad(const void* grad_rows, int32_t dtype, int32_t n, int32_t 
 int64_t rollout_head_logprobs_workspace(int32_t rows, int32_t vocab, int32_t hidden) {
   return bytes_of([&] {
     check_sizes(rows, vocab, hidden);
+    check_product(rows, hidden);
+    check_tiles(rows, vocab);
     return head_workspace(rows, vocab, hidden);
   });
 }
@@ -221,6 +260,8 @@ int rollout_head_logprobs(const void* hidden_states, int64_t hidden_stride, cons
 int64_t rollout_head_logprobs_grad_workspace(int32_t rows, int32_t vocab, int32_t hidden) {
   return bytes_of([&] {
     check_sizes(rows, vocab, hidden);
+    check_product(rows, hidden);
+    check_tiles(rows, vocab);
     return head_grad_workspace(rows, vocab, hidden);
   });
 }
@@ -237,6 +278,13 @@ int rollout_head_logprobs_grad(const void* hidden_states, int64_t hidden_stride,
       check_array(grad_hidden, 16, "grad_hidden");
       check_gradients(row_stats, entropy, grad_logp, grad_entropy);
     }
+    const Extent states = extent(hidden_states, rows, hidden, hidden_stride, 2), head = extent(lm_head, vocab, hidden, head_stride, 2);
+    const Extent d_states = extent(grad_hidden, rows, hidden, hidden, 2), d_head = extent(grad_head, vocab, hidden, hidden, 2);
+    check_apart(states, d_states, "hidden_states and grad_hidden");
+    check_apart(states, d_head, "hidden_states and grad_head");
+    check_apart(head, d_states, "lm_head and grad_hidden");
+    check_apart(head, d_head, "lm_head and grad_head");
+    check_apart(d_states, d_head, "grad_hidden and grad_head");
     check_workspace(workspace, workspace_bytes, head_grad_workspace(rows, vocab, hidden));
     const HeadGrad a{in, row_stats, entropy, grad_logp, grad_entropy, grad_hidden, grad_head};
     enqueue([&] { launch_head_logprobs_grad(a, workspace, (hipStream_t)hip_stream); });

@@ -234,6 +234,24 @@ def test_in_place(dtype):
     assert (buf[1 + 3333:1 + 3340] == 77.0).all()
 
 
+def test_gradients_beside_their_logits():
+    import torch
+    import paper_2506_06122_amd as R
+    wide = torch.full((6, 2 * 1001 + 3), 7.0, device="cuda")
+    x, out = wide[:, :1001], wide[:, 1003:2004]
+    x.copy_(torch.from_numpy(make("plain", 6, 1001, 8)))
+    t = targets_of(6, 1001, 8)
+    got = R.rollout_token_logprobs(x, cuda(t))
+    g, h = grads_of(6, 8, True)
+    want = R.rollout_token_logprobs_grad(x, cuda(t), got[2], got[1], cuda(g), cuda(h))
+    held = x.clone()
+    R.rollout_token_logprobs_grad(x, cuda(t), got[2], got[1], cuda(g), cuda(h), out=out)
+    assert torch.equal(out, want) and torch.equal(x, held)
+    assert (wide[:, 1001:1003] == 7.0).all() and (wide[:, 2004:] == 7.0).all()
+    with pytest.raises(R.RolloutError):
+        R.rollout_token_logprobs_grad(x, cuda(t), got[2], got[1], cuda(g), cuda(h), out=wide[:, 1000:2001])
+
+
 def test_rows_past_32_bits():
     import torch
     import paper_2506_06122_amd as R

@@ -7,7 +7,7 @@ import torch
 import paper_2506_06122_amd as R
 from paper_2506_06122_amd import binding as B
 
-ARRAY = 4096  # an aligned address that is never read
+ARRAY, OTHER, THIRD, FOURTH = (k << 24 for k in (1, 2, 3, 4))  # aligned addresses, far apart, that are never read
 
 
 def call(name, args, **changed):
@@ -24,16 +24,16 @@ TOKENS = dict(logits=ARRAY, dtype=1, rows=3, vocab=100, row_stride=100, temperat
               workspace=None, workspace_bytes=0, stream=None, logp=ARRAY, entropy=ARRAY, row_stats=ARRAY, top_ids=ARRAY,
               top_logp=ARRAY)
 GRAD = dict(logits=ARRAY, dtype=1, rows=3, vocab=100, row_stride=100, temperature=1.0, targets=ARRAY, row_stats=ARRAY,
-            entropy=ARRAY, grad_logp=ARRAY, grad_entropy=ARRAY, stream=None, grad_logits=2 * ARRAY, grad_row_stride=100)
-EMBED = dict(table=ARRAY, dtype=1, vocab=100, hidden=64, table_stride=64, tokens=ARRAY, n=3, scale=1.0, stream=None, out=ARRAY)
+            entropy=ARRAY, grad_logp=ARRAY, grad_entropy=ARRAY, stream=None, grad_logits=OTHER, grad_row_stride=100)
+EMBED = dict(table=ARRAY, dtype=1, vocab=100, hidden=64, table_stride=64, tokens=ARRAY, n=3, scale=1.0, stream=None, out=OTHER)
 EMBED_GRAD = dict(grad_rows=ARRAY, dtype=1, n=3, vocab=100, hidden=64, row_stride=64, tokens=ARRAY, scale=1.0, base=None,
-                  table_dtype=1, workspace=ARRAY, workspace_bytes=1 << 20, stream=None, grad_table=ARRAY)
+                  table_dtype=1, workspace=ARRAY, workspace_bytes=1 << 20, stream=None, grad_table=OTHER)
 
 HEAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stride=64, rows=3, vocab=100, hidden=64, temperature=1.0,
             targets=ARRAY, workspace=ARRAY, workspace_bytes=1 << 20, stream=None, logp=ARRAY, entropy=ARRAY, row_stats=ARRAY)
-HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stride=64, rows=3, vocab=100, hidden=64,
+HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=OTHER, head_stride=64, rows=3, vocab=100, hidden=64,
                  temperature=1.0, targets=ARRAY, row_stats=ARRAY, entropy=ARRAY, grad_logp=ARRAY, grad_entropy=ARRAY,
-                 workspace=ARRAY, workspace_bytes=1 << 20, stream=None, grad_hidden=ARRAY, grad_head=ARRAY)
+                 workspace=ARRAY, workspace_bytes=1 << 20, stream=None, grad_hidden=THIRD, grad_head=FOURTH)
 
 
 @pytest.mark.parametrize("name,args,changed,word", [
@@ -65,6 +65,10 @@ HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stri
     ("rollout_token_logprobs_grad", GRAD, dict(grad_logits=None), "grad_logits"),
     ("rollout_token_logprobs_grad", GRAD, dict(grad_row_stride=99), "grad_row_stride"),
     ("rollout_token_logprobs_grad", GRAD, dict(grad_logits=ARRAY, grad_row_stride=101), "in place"),
+    ("rollout_token_logprobs_grad", GRAD, dict(grad_logits=ARRAY + 2), "overlap"),
+    ("rollout_token_logprobs_grad", GRAD, dict(grad_logits=ARRAY + 400, grad_row_stride=150), "overlap"),
+    ("rollout_token_logprobs_grad", GRAD, dict(row_stride=200, grad_row_stride=200, grad_logits=ARRAY + 2 * 99), "overlap"),
+    ("rollout_token_logprobs_grad", GRAD, dict(row_stride=200, grad_row_stride=200, grad_logits=ARRAY + 2 * 101), "overlap"),
     ("rollout_token_logprobs_grad", GRAD, dict(row_stats=None), "row_stats"),
     ("rollout_token_logprobs_grad", GRAD, dict(grad_logp=None), "grad_logp"),
     ("rollout_token_logprobs_grad", GRAD, dict(entropy=None), "entropy"),
@@ -77,6 +81,10 @@ HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stri
     ("rollout_embed", EMBED, dict(table_stride=63), "table_stride"),
     ("rollout_embed", EMBED, dict(scale=float("inf")), "scale"),
     ("rollout_embed", EMBED, dict(n=-1), "rows"),
+    ("rollout_embed", EMBED, dict(out=ARRAY + 2 * 64 * 99), "overlap"),
+    ("rollout_embed", EMBED, dict(n=1 << 24, hidden=1 << 20, table_stride=1 << 20), "2^38"),
+    ("rollout_embed_grad", EMBED_GRAD, dict(base=OTHER + 2), "overlap"),
+    ("rollout_embed_grad", EMBED_GRAD, dict(grad_rows=OTHER + 128), "overlap"),
     ("rollout_embed_grad", EMBED_GRAD, dict(grad_rows=None), "grad_rows"),
     ("rollout_embed_grad", EMBED_GRAD, dict(tokens=None), "tokens"),
     ("rollout_embed_grad", EMBED_GRAD, dict(grad_table=None), "grad_table"),
@@ -114,6 +122,10 @@ HEAD_GRAD = dict(hidden_states=ARRAY, hidden_stride=64, lm_head=ARRAY, head_stri
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_hidden=None), "grad_hidden"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_head=ARRAY + 8), "aligned"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(entropy=None), "entropy"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_head=OTHER), "overlap"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_hidden=ARRAY), "overlap"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_hidden=FOURTH + 64 * 99 * 2), "overlap"),
+    ("rollout_head_logprobs", HEAD, dict(rows=1 << 24, vocab=1 << 24), "2^42"),
     ("rollout_head_logprobs_grad", HEAD_GRAD, dict(grad_logp=None), "grad_logp"),
 ])
 def test_refused(name, args, changed, word):
