@@ -84,7 +84,10 @@ constexpr HeadBlock head_block(unsigned index, const HeadGrid& g) {
   return HeadBlock{m, n, z, m < g.m_tiles && n < g.n_tiles && z < g.splits};
 }
 
-// Rows and columns of the tiles that an M x N product is cut into
+// Rows and columns of the tiles that an M x N product is cut into.  More than 128 rows take tiles of 160 to 256 rows, so that
+// neither the last row of tiles nor the last round of 256 workgroups stands half empty: a round costs as much as its
+// rows and some 150 more (151936 x 1536: 160 rows in one tile 138 us, in two of 128 161; 300 in two of 160 196, in two of
+// 256 236; 613 in three of 224 316, of 256 345; 512 in two of 256 239, in three of 192 286).
 struct HeadTile {
   int m, n;
 };
@@ -92,12 +95,27 @@ constexpr HeadTile head_tile(int M, int N) {
   if (M <= 16) return {16, 256};
   if (M <= 32) return {32, 256};
   if (M <= 64) return {64, 256};
+  const int across = head_ceil(N, 256);
+  if (M <= 128 || head_ceil(M, 160) * (long long)across < 192) return {128, 128};
+  int best = 256;
+  long long best_time = 0;
+  for (int m = 256; m >= 160; m -= 32) {
+    const long long time = (long long)head_ceil((long long)head_ceil(M, m) * across, 256) * (m + 150);
+    if (m == 256 || time < best_time) {
+      best_time = time;
+      best = m;
+    }
+  }
+  return {best, 256};
+}
+// the gradients' first product writes whole slices of rows, zeros included (16 x 256 tiles, 7 rows: 208 us, four times the
+// workgroups, where 64 x 256 take 119), and the device alone knows how many rows there are (160 rows, a quarter without
+// gradient, 151936 x 1536, all three products: 445 us with 128 x 128 tiles here, 474 with 256 x 256)
+constexpr HeadTile head_tile_logits(int M, int N) {
+  if (M <= 64) return {64, 256};
   if (M <= 256 || head_ceil(M, 256) * (long long)head_ceil(N, 256) < 192) return {128, 128};
   return {256, 256};
 }
-// the gradients' first product writes whole slices of rows, zeros included (16 x 256 tiles, 7 rows: 208 us, four times the
-// workgroups)
-constexpr HeadTile head_tile_logits(int M, int N) { return head_tile(head_max(M, 64), N); }
 // the gradients' second and third product: K is long in grad_hidden's, which is cut along it instead, and short in
 // grad_head's with few rows, where two small workgroups to a CU hide each other's start and end (7 rows 498 -> 470 us
 // in all, 187 rows 600 -> 576, but 613 rows 900 -> 940)

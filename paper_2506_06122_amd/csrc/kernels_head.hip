@@ -460,6 +460,11 @@ template <int TO, bool AK, bool BK>
 void launch_product(const Product& p, HeadTile t, int blocks, hipStream_t s) {
   if (t.m == 256) return launch_shape<2, 2, 8, 8, 2, TO, AK, BK>(p, blocks, s);
   if (t.m == 128) return launch_shape<2, 2, 4, 4, 2, TO, AK, BK>(p, blocks, s);
+  if constexpr (TO == TO_SUMS) {
+    if (t.m == 160) return launch_shape<2, 2, 5, 8, 2, TO, AK, BK>(p, blocks, s);
+    if (t.m == 192) return launch_shape<2, 2, 6, 8, 2, TO, AK, BK>(p, blocks, s);
+    if (t.m == 224) return launch_shape<2, 2, 7, 8, 2, TO, AK, BK>(p, blocks, s);
+  }
   if constexpr (!BK) {  // products that walk over W by its rows
     if (t.m == 64) return launch_shape<1, 4, 4, 4, 2, TO, AK, BK>(p, blocks, s);
     if constexpr (TO == TO_SUMS) {

@@ -93,6 +93,9 @@ static void by_tile(const Product& p) {
   else if (t.m == 32 && t.n == 256) walk<32, 256, AK, BK>(p);
   else if (t.m == 64 && t.n == 256) walk<64, 256, AK, BK>(p);
   else if (t.m == 128 && t.n == 128) walk<128, 128, AK, BK>(p);
+  else if (t.m == 160 && t.n == 256 && !AK && !BK) walk<160, 256, AK, BK>(p);
+  else if (t.m == 192 && t.n == 256 && !AK && !BK) walk<192, 256, AK, BK>(p);
+  else if (t.m == 224 && t.n == 256 && !AK && !BK) walk<224, 256, AK, BK>(p);
   else if (t.m == 256 && t.n == 256) walk<256, 256, AK, BK>(p);
   else bad("unknown tile", p.name, t.m, t.n, 0, 0);
 }
@@ -159,13 +162,16 @@ int main() {
   fragments<32, false>();
   fragments<64, false>();
   fragments<128, false>();
+  fragments<160, false>();
+  fragments<192, false>();
+  fragments<224, false>();
   fragments<256, false>();
   fragments<16, true>();
   fragments<32, true>();
   fragments<64, true>();
   fragments<128, true>();
   fragments<256, true>();
-  for (int rows : {1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 613, 1500, 4096, 70001})
+  for (int rows : {1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 160, 187, 255, 256, 257, 300, 400, 511, 613, 1500, 4096, 70001})
     for (int vocab : {1, 33, 100, 256, 257, 513, 4099, 32001, 152064})
       for (int hidden : {64, 192, 1536, 3584})
         sizes(rows, vocab, hidden, hidden % 128 ? 8 : 0);

@@ -106,7 +106,8 @@ def test_tiles_of_every_size_agree_with_the_logits_path():
     """Large enough for the largest tiles, checked against float64 products on the GPU and the logits' own operator."""
     import torch
     import paper_2506_06122_amd as R
-    for rows, vocab, hidden in ((1500, 12301, 192), (4096, 4099, 64), (513, 30001, 1536)):
+    for rows, vocab, hidden in ((1500, 12301, 192), (4096, 4099, 64), (513, 30001, 1536), (150, 50257, 128), (190, 50257, 64),
+                                (310, 32001, 128), (430, 50257, 64)):
         h, w, t = inputs(rows, vocab, hidden, 5)
         g, e = map(cuda, grads_of(rows, 5, True))
         x = h.double() @ w.double().T
