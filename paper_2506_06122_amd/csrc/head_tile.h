@@ -144,6 +144,8 @@ constexpr int head_splits(int tiles, int k_tiles, HeadTile t) {
 // the gradients are kept as a bf16 value and the bf16 rest, below the first values' rows: twice the rows for
 // grad_hidden's product, twice the K for grad_head's, which few rows do not notice much.
 constexpr int kHeadTwoPlanes = 128;  // rows up to which
+// a plane's rows are padded to this, so that all planes are whole slices
+constexpr int head_pad(int planes) { return kHeadDeep / planes; }
 struct HeadGradPlan {
   int rows;    // room for the rows of the logits' gradients: a whole number of slices
   int planes;  // 1 or 2
@@ -161,12 +163,11 @@ constexpr HeadGradPlan head_grad_plan(int rows, int vocab) {
 // What `count` rows with a gradient make of it, known to the device only
 struct HeadActive {
   int count;   // rows
-  int stacked; // rows of the logits' gradients as the products see them: the planes below each other, each a whole number
-               // of slices (zeros in between)
+  int stacked; // rows of the logits' gradients as the products see them: the planes below each other, padded with zeros
   int splits;  // of K in grad_hidden's product
 };
 constexpr HeadActive head_active(int count, const HeadGradPlan& g, int vocab, int hidden) {
-  HeadActive a{count, g.planes == 1 ? count : 2 * head_up(count, kHeadDeep), 1};
+  HeadActive a{count, g.planes == 1 ? count : 2 * head_up(count, head_pad(2)), 1};
   // (the tile is chosen by the rows there is room for: the launch does not know the count)
   const HeadTile t = head_tile_hidden(g.rows * g.planes);
   const int tiles = head_ceil(a.stacked, t.m) * head_ceil(hidden, t.n), slices = head_ceil(head_min(vocab, g.chunk), kHeadDeep);
@@ -215,10 +216,10 @@ struct HeadExtent {
   int a_limit, b_limit;  // rows or columns of the slices that exist, from the tile's first
   int b_last;            // steps of B's last slice that exist
 };
-constexpr HeadExtent head_extent(bool a_km, bool b_km, bool pad_rows, int m0, int n0, int z, int M, int N, int K, int per_split,
+constexpr HeadExtent head_extent(bool a_km, bool b_km, int pad, int m0, int n0, int z, int M, int N, int K, int per_split,
                                  int row_capacity) {
   HeadExtent x{};
-  x.m_end = pad_rows ? head_min(row_capacity, head_up(M, kHeadDeep)) : M;
+  x.m_end = pad ? head_min(row_capacity, head_up(M, pad)) : M;
   x.k_tiles = head_ceil(K, kHeadDeep);
   x.kt_begin = z * per_split;
   x.kt_end = head_min(x.k_tiles, x.kt_begin + per_split);

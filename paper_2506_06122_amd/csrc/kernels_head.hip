@@ -119,13 +119,14 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
   const int r = lane & 15, g = lane >> 4;
   const int M = TO == TO_GRAD ? p.plan->count : TO == TO_PLANE ? p.plan->stacked : p.M, K = TO == TO_BF16 ? p.plan->stacked : p.K;
   HeadGrid grid = p.grid;
-  if constexpr (TO == TO_GRAD || TO == TO_PLANE) grid = head_grid_rows(grid, head_ceil(TO == TO_GRAD ? head_up(M, kHeadDeep) : M, BM));
+  const int pad = TO == TO_GRAD ? head_pad(p.planes) : 0, rows = TO == TO_GRAD ? head_up(M, pad) : M;
+  if constexpr (TO == TO_GRAD || TO == TO_PLANE) grid = head_grid_rows(grid, head_ceil(rows, BM));
   if constexpr (TO == TO_PLANE) grid.splits = p.plan->splits;
   const HeadBlock block = head_block(blockIdx.x, grid);
   if (!block.inside) return;
   const int bn = block.n, bz = block.z;
   const int m0 = block.m * BM, n0 = bn * BN;
-  const HeadExtent x = head_extent(AK, BK, TO == TO_GRAD, m0, n0, bz, M, p.N, K, TO == TO_PLANE ? head_ceil(head_ceil(K, kHeadDeep), grid.splits) : head_ceil(K, kHeadDeep),
+  const HeadExtent x = head_extent(AK, BK, pad, m0, n0, bz, M, p.N, K, TO == TO_PLANE ? head_ceil(head_ceil(K, kHeadDeep), grid.splits) : head_ceil(K, kHeadDeep),
                                    p.row_capacity);
   if (m0 >= x.m_end) return;
   const int k_tiles = x.k_tiles, kt_begin = x.kt_begin, kt_end = x.kt_end;
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
   } else {
     // bf16, through LDS so that rows leave as whole lines
     char* mine = lds + wave * OUT_WAVE;
-    const RowGrad* rows = (const RowGrad*)(lds + OUT);
+    const RowGrad* row_grads = (const RowGrad*)(lds + OUT);
     const float c = p.inv_temp * kLog2e;
     if constexpr (TO == TO_GRAD) {
       for (int ml = threadIdx.x; ml < BM; ml += NW * 64) {
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       if constexpr (TO == TO_GRAD) {
-        const RowGrad q = rows[(wm * MT + i) * 16 + r];
+        const RowGrad q = row_grads[(wm * MT + i) * 16 + r];
         const int from = q.target - p.col0 - col0, place = (from >> 4) * 4 + (from & 3);
         const bool here = q.target >= 0 && from >= 0 && from < NT * 16 && (from >> 2 & 3) == g;
 #pragma unroll
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
         const u32x4 w = *(const u32x4*)(mine + ml * OUT_ROW + lane % LANES * 16);
         if (m < x.m_end && n < n_end) *(u32x4*)(out + m * out_pitch) = w;
       }
-      out += head_up(M, kHeadDeep) * out_pitch;
+      out += rows * out_pitch;
     }
   }
 }
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(1024) void head_active_kernel(HeadGrad a, HeadGradP
 }
 // The rows of hidden_states that go with the stacked gradients, zeros in between; one row per workgroup
 __global__ __launch_bounds__(256) void head_gather_kernel(HeadArgs in, int planes, const HeadActive* plan, const int* active, uint16_t* out) {
-  const int n = plan->count, rows = head_up(n, kHeadDeep), row = blockIdx.x;
+  const int n = plan->count, rows = head_up(n, head_pad(planes)), row = blockIdx.x;
   if (row >= rows * planes) return;
   const int i = row >= rows ? row - rows : row;
   const u32x4* src = i < n ? (const u32x4*)((const uint16_t*)in.hidden_states + active[i] * in.hidden_stride) : nullptr;

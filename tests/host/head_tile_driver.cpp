@@ -20,7 +20,7 @@ struct Array {
 struct Product {
   const char* name;
   HeadTile tile;
-  bool pad_rows;
+  int pad_rows;
   Array a, b, out;
   long long a_pitch, b_pitch, out_pitch, out_size;
   int m_room, M, N, K, capacity, splits, blocks;  // M, K, splits: as the device finds them
@@ -46,7 +46,7 @@ template <int BM, int BN, bool AK, bool BK>
 static void walk(const Product& p) {
   const int M = p.M, K = p.K, per = p.splits > 1 ? head_ceil(head_ceil(K, kHeadDeep), p.splits) : head_ceil(K, kHeadDeep);
   const HeadGrid room = head_grid(head_ceil(p.pad_rows ? p.capacity : p.m_room, BM), head_ceil(p.N, BN), 1);
-  const int m_tiles = head_ceil(p.pad_rows ? head_up(M, kHeadDeep) : M, BM), n_tiles = room.n_tiles, tiles = m_tiles * n_tiles * p.splits;
+  const int m_tiles = head_ceil(p.pad_rows ? head_up(M, p.pad_rows) : M, BM), n_tiles = room.n_tiles, tiles = m_tiles * n_tiles * p.splits;
   const int blocks = p.blocks ? p.blocks : head_blocks(room);
   HeadGrid grid = head_grid_rows(room, m_tiles);
   grid.splits = p.splits;
@@ -103,7 +103,7 @@ static void by_tile(const Product& p) {
 static void sizes(int rows, int vocab, int hidden, int pad) {
   const long long hp = hidden + pad;
   const Array states{(rows - 1) * hp * 2 + hidden * 2}, head{(vocab - 1) * hp * 2 + hidden * 2ll};
-  by_tile<false, false>({"logits", head_tile(rows, vocab), false, states, head, {0}, hp, hp, 0, 0, rows, rows, vocab, hidden, 0, 1, 0, 0, false, 0});
+  by_tile<false, false>({"logits", head_tile(rows, vocab), 0, states, head, {0}, hp, hp, 0, 0, rows, rows, vocab, hidden, 0, 1, 0, 0, false, 0});
   const HeadGradPlan g = head_grad_plan(rows, vocab);
   const HeadMost most = head_most(g, rows, vocab, hidden);
   const int room = g.rows * g.planes;
@@ -118,10 +118,10 @@ static void sizes(int rows, int vocab, int hidden, int pad) {
       const int v = head_min(g.chunk, vocab - v0);
       const Array w{(long long)(v - 1) * hp * 2 + hidden * 2ll + (long long)(vocab - v0 - v) * hp * 2};
       for (int plane = 0; plane < g.planes; ++plane)
-        by_tile<false, false>({"gradients", head_tile_logits(rows, v), true, h, w, dx, hidden, hp, 0, 2, rows, count, v, hidden, g.rows, 1, 0,
-                               (long long)plane * head_up(count, kHeadDeep), false, room});
-      by_tile<false, true>({"grad_hidden", head_tile_hidden(room), false, dx, w, parts, kHeadPanel, hp, hidden, 4, room, a.stacked, hidden, v, 0, a.splits, most.blocks, 0, true, room});
-      by_tile<true, true>({"grad_head", head_tile_head(rows), false, dx, h, {(long long)v * hidden * 2}, kHeadPanel, hidden, hidden, 2, v, v, hidden, a.stacked, 0, 1, 0, 0, true, room});
+        by_tile<false, false>({"gradients", head_tile_logits(rows, v), head_pad(g.planes), h, w, dx, hidden, hp, 0, 2, rows, count, v, hidden, g.rows, 1, 0,
+                               (long long)plane * head_up(count, head_pad(g.planes)), false, room});
+      by_tile<false, true>({"grad_hidden", head_tile_hidden(room), 0, dx, w, parts, kHeadPanel, hp, hidden, 4, room, a.stacked, hidden, v, 0, a.splits, most.blocks, 0, true, room});
+      by_tile<true, true>({"grad_head", head_tile_head(rows), 0, dx, h, {(long long)v * hidden * 2}, kHeadPanel, hidden, hidden, 2, v, v, hidden, a.stacked, 0, 1, 0, 0, true, room});
     }
   }
 }
