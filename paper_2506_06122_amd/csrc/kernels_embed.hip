@@ -16,7 +16,7 @@ namespace {
 
 // ---- lookup --------------------------------------------------------------------------------
 // One thread per 16 bytes of the result (VEC), or per value where rows are not whole, aligned vectors.
-template <typename V, bool VEC>
+template <typename V, bool VEC, bool STREAM>
 __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedArgs a, int per_row) {
   constexpr int E = VEC ? kVec<V> : 1;
   const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -39,7 +39,8 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedArgs a, int per_ro
         w = narrow(v, V{});
       }
     }
-    *(u32x4*)dst = w;
+    if constexpr (STREAM) __builtin_nontemporal_store(w, (u32x4*)dst);
+    else *(u32x4*)dst = w;
   } else {
     *dst = !inside ? narrow1(0.f, V{}) : a.scale == 1.f ? *src : narrow1(to_f32(*src) * a.scale, V{});
   }
@@ -51,8 +52,10 @@ void launch_rows(const EmbedArgs& a, hipStream_t s) {
   const bool vec = a.hidden % E == 0 && a.table_stride % E == 0 && (((size_t)a.table | (size_t)a.out) & 15) == 0;
   const int per_row = vec ? a.hidden / E : a.hidden;
   const int grid = ceil_div((long long)a.n * per_row, 256);
-  if (vec) embed_rows_kernel<V, true><<<grid, 256, 0, s>>>(a, per_row);
-  else embed_rows_kernel<V, false><<<grid, 256, 0, s>>>(a, per_row);
+  const bool stream = (long long)a.n * a.hidden * sizeof(V) > kLastCache / 4;
+  if (vec && stream) embed_rows_kernel<V, true, true><<<grid, 256, 0, s>>>(a, per_row);
+  else if (vec) embed_rows_kernel<V, true, false><<<grid, 256, 0, s>>>(a, per_row);
+  else embed_rows_kernel<V, false, false><<<grid, 256, 0, s>>>(a, per_row);
 }
 
 // ---- gradient ------------------------------------------------------------------------------

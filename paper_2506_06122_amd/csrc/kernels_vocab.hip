@@ -331,9 +331,12 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
 
 // dx_v = [g (1{v = t} - p_v) - h p_v (ln p_v + H)] / T, value by value; a row without a gradient is written without being
 // read.  SAME: rows of both arrays lie alike relative to 16 bytes.
-template <typename V, bool SAME>
+//
+// Bound by memory: a thread takes one vector, so that the workgroups that run at a time read and write neighbouring
+// addresses, and what is larger than the last cache is passed by it (STREAM).  6144 x 152064 bf16: see launch_grad.
+template <typename V, bool SAME, bool STREAM>
 __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
-  constexpr int E = kVec<V>, U = 4;
+  constexpr int E = kVec<V>;
   const int tid = threadIdx.x, r = blockIdx.x / parts, part = blockIdx.x % parts;
   const RowSlice<V> row((const V*)a.in.logits + r * a.in.stride, a.in.vocab, part, parts);
   V* out = (V*)a.out + r * a.out_stride;
@@ -341,7 +344,10 @@ __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
   const float c = a.in.inv_temp * kLog2e;
   auto store = [&](int i, const float* v) {
     if constexpr (SAME) {
-      *(u32x4*)(out + row.id(i)) = narrow(v, V{});
+      u32x4* to = (u32x4*)(out + row.id(i));
+      const u32x4 w = narrow(v, V{});
+      if constexpr (STREAM) __builtin_nontemporal_store(w, to);
+      else *to = w;
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) out[row.id(i) + e] = narrow1(v[e], V{});
@@ -354,9 +360,9 @@ __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
     if (one >= 0) out[one] = narrow1(0.f, V{});
     return;
   }
-  auto apply = [&](u32x4 w, int i) {
+  for (int i = row.begin + tid; i < row.end; i += T) {
     float v[E];
-    widen(w, v, V{});
+    widen(STREAM ? __builtin_nontemporal_load((const u32x4*)(row.x + row.id(i))) : row.vec(i), v, V{});
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] = grad_of(v[e], c, g);
     const unsigned at = (unsigned)(g.target - row.id(i));
@@ -365,16 +371,7 @@ __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
       for (int e = 0; e < E; ++e) v[e] += at == e ? g.at_target : 0.f;
     }
     store(i, v);
-  };
-  int i = row.begin + tid;
-  for (; i + (U - 1) * T < row.end; i += U * T) {
-    u32x4 w[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = row.vec(i + u * T);
-#pragma unroll
-    for (int u = 0; u < U; ++u) apply(w[u], i + u * T);
   }
-  for (; i < row.end; i += T) apply(row.vec(i), i);
   if (one >= 0) out[one] = narrow1(grad_of(to_f32(row.x[one]), c, g) + (one == g.target ? g.at_target : 0.f), V{});
 }
 
@@ -397,12 +394,17 @@ void launch(const TokenRows& in, const TokenOut& out, const TokenParts& p, hipSt
 }
 
 template <typename V>
-void launch_grad(const TokenGrad& a, int parts, hipStream_t s) {
+void launch_grad(const TokenGrad& a, hipStream_t s) {
   const size_t size = sizeof(V);
   const bool same = (((size_t)a.in.logits - (size_t)a.out) & 15) == 0 && ((a.in.stride - a.out_stride) * size & 15) == 0;
+  const bool stream = (long long)a.in.rows * a.in.vocab * size > kLastCache;
+  // a vector to a thread, as long as the workgroups can be counted
+  int parts = std::max(1, ceil_div(a.in.vocab, T * kVec<V>));
+  while ((long long)a.in.rows * parts > 0x7fffffff) parts = (parts + 1) / 2;
   const int grid = a.in.rows * parts;
-  if (same) token_grad_kernel<V, true><<<grid, T, 0, s>>>(a, parts);
-  else token_grad_kernel<V, false><<<grid, T, 0, s>>>(a, parts);
+  if (same && stream) token_grad_kernel<V, true, true><<<grid, T, 0, s>>>(a, parts);
+  else if (same) token_grad_kernel<V, true, false><<<grid, T, 0, s>>>(a, parts);
+  else token_grad_kernel<V, false, false><<<grid, T, 0, s>>>(a, parts);
 }
 
 }  // namespace
@@ -423,8 +425,7 @@ void launch_token_logprobs(const TokenRows& in, const TokenOut& out, void* ws, h
   else launch<f16_t>(in, out, p, s);
 }
 void launch_token_logprobs_grad(const TokenGrad& a, hipStream_t s) {
-  const int parts = token_parts(a.in.rows, a.in.vocab);
-  if (a.in.dtype == VT_F32) launch_grad<float>(a, parts, s);
-  else if (a.in.dtype == VT_BF16) launch_grad<bf16_t>(a, parts, s);
-  else launch_grad<f16_t>(a, parts, s);
+  if (a.in.dtype == VT_F32) launch_grad<float>(a, s);
+  else if (a.in.dtype == VT_BF16) launch_grad<bf16_t>(a, s);
+  else launch_grad<f16_t>(a, s);
 }

@@ -8,6 +8,8 @@
 enum { VT_F32 = 0, VT_BF16 = 1, VT_F16 = 2 };
 constexpr size_t vt_size(int dtype) { return dtype == VT_F32 ? 4 : 2; }
 
+constexpr long long kLastCache = 256ll << 20;  // bytes of the cache before memory
+
 constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
 
 // ---- logits ------------------------------------------------------------------------------
