@@ -93,7 +93,7 @@ EmbedPlan plan(int n, int vocab) {
 // walk puts them there: the order within an id is the order of the rows, and no workgroup waits for another.  The
 // workgroups behind them fill the matrix.
 template <typename G>
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, EmbedSort q, int ranges, int range, bool fill) {
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, EmbedSort q, int ranges, int range, bool fill, bool stream) {
   __shared__ int count_s[kSortWaves][kRange];
   __shared__ int below_s[kSortWaves], scan_s[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -113,9 +113,16 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, E
     const u32x4* b = (const u32x4*)(base + head);
     const u32x4 none = {0, 0, 0, 0};
     const long long first = block * kFill + tid, end = min(vecs, (block + 1) * (long long)kFill);
-    if (!base) {
+    // what is larger than the last cache passes it by (152064 x 3584 in bf16, the whole call: 248 -> 232 us)
+    if (!base && stream) {
+#pragma unroll 4
+      for (long long i = first; i < end; i += kSortThreads) __builtin_nontemporal_store(none, o + i);
+    } else if (!base) {
 #pragma unroll 4
       for (long long i = first; i < end; i += kSortThreads) o[i] = none;
+    } else if (stream && (((size_t)base - (size_t)out) & 15) == 0) {
+#pragma unroll 4
+      for (long long i = first; i < end; i += kSortThreads) __builtin_nontemporal_store(__builtin_nontemporal_load(b + i), o + i);
     } else if ((((size_t)base - (size_t)out) & 15) == 0) {
 #pragma unroll 4
       for (long long i = first; i < end; i += kSortThreads) o[i] = b[i];
@@ -318,7 +325,7 @@ void launch_grad(const EmbedGrad& a, void* ws, hipStream_t s) {
   const bool fill = a.base != a.out;
   const long long bytes = (long long)a.vocab * a.hidden * sizeof(G);
   const int fillers = fill ? ceil_div(bytes, kFill * 16) : 0;
-  embed_sort_kernel<G><<<p.ranges + fillers, kSortThreads, 0, s>>>(a, q, p.ranges, p.range, fill);
+  embed_sort_kernel<G><<<p.ranges + fillers, kSortThreads, 0, s>>>(a, q, p.ranges, p.range, fill, bytes > kLastCache);
   if (p.chunks == 0) return;
   // whole vectors of 8 values: every row starts on 16 bytes
   const bool vec = a.hidden % 8 == 0 && a.row_stride % 8 == 0 && (((size_t)a.grad_rows | (size_t)a.base | (size_t)a.out) & 15) == 0;

@@ -333,7 +333,8 @@ __global__ __launch_bounds__(T) void token_join_kernel(TokenRows in, TokenOut ou
 // read.  SAME: rows of both arrays lie alike relative to 16 bytes.
 //
 // Bound by memory: a thread takes one vector, so that the workgroups that run at a time read and write neighbouring
-// addresses, and what is larger than the last cache is passed by it (STREAM).  6144 x 152064 bf16: see launch_grad.
+// addresses, and what is larger than the last cache passes it by (STREAM).  6144 x 152064 bf16, all rows with a
+// gradient: 601 us, 6.2 TB/s; with four vectors to a thread, through the caches, 736.
 template <typename V, bool SAME, bool STREAM>
 __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
   constexpr int E = kVec<V>;
