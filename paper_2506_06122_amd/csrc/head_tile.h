@@ -84,7 +84,9 @@ constexpr HeadBlock head_block(unsigned index, const HeadGrid& g) {
   return HeadBlock{m, n, z, m < g.m_tiles && n < g.n_tiles && z < g.splits};
 }
 
-// Rows and columns of the tiles that an M x N product is cut into.  More than 128 rows take tiles of 160 to 256 rows, so that
+// Rows and columns of the tiles that an M x N product is cut into.  Up to 128 rows are one tile, so that W is read once
+// (128 x 152064 x 3584: 219 us, in 128 x 128 tiles 245), unless that leaves many CUs without one (128 x 32000 x 4096: 55 us,
+// in 128 x 128 tiles 52).  More than 128 rows take tiles of 160 to 256 rows, so that
 // neither the last row of tiles nor the last round of 256 workgroups stands half empty: a round costs as much as its
 // rows and some 150 more (151936 x 1536: 160 rows in one tile 138 us, in two of 128 161; 300 in two of 160 196, in two of
 // 256 236; 613 in three of 224 316, of 256 345; 512 in two of 256 239, in three of 192 286).
@@ -96,6 +98,7 @@ constexpr HeadTile head_tile(int M, int N) {
   if (M <= 32) return {32, 256};
   if (M <= 64) return {64, 256};
   const int across = head_ceil(N, 256);
+  if (M <= 128 && across >= 192) return {128, 256};
   if (M <= 128 || head_ceil(M, 160) * (long long)across < 192) return {128, 128};
   int best = 256;
   long long best_time = 0;
@@ -110,22 +113,25 @@ constexpr HeadTile head_tile(int M, int N) {
 }
 // the gradients' first product writes whole slices of rows, zeros included (16 x 256 tiles, 7 rows: 208 us, four times the
 // workgroups, where 64 x 256 take 119), and the device alone knows how many rows there are (160 rows, a quarter without
-// gradient, 151936 x 1536, all three products: 445 us with 128 x 128 tiles here, 474 with 256 x 256)
+// gradient, 151936 x 1536, all three products: 445 us with 128 x 128 tiles here, 474 with 256 x 256; 128 x 256 1 to 2 %
+// less than 128 x 128: 187 rows 477 -> 468, 128 rows x 152064 x 3584 968 -> 956)
 constexpr HeadTile head_tile_logits(int M, int N) {
   if (M <= 64) return {64, 256};
+  if (M <= 256 && head_ceil(N, 256) >= 192) return {128, 256};
   if (M <= 256 || head_ceil(M, 256) * (long long)head_ceil(N, 256) < 192) return {128, 128};
   return {256, 256};
 }
 // the gradients' second and third product: K is long in grad_hidden's, which is cut along it instead, and short in
-// grad_head's with few rows, where two small workgroups to a CU hide each other's start and end (7 rows 498 -> 470 us
-// in all, 187 rows 600 -> 576, but 613 rows 900 -> 940)
-constexpr HeadTile head_tile_hidden(int M) { return M <= 256 ? HeadTile{128, 128} : HeadTile{256, 256}; }
-constexpr HeadTile head_tile_head(int K) { return K <= 256 ? HeadTile{128, 128} : HeadTile{256, 256}; }
+// grad_head's with few rows, where two small workgroups to a CU hide each other's start and end (32 rows x 152064 x 3584 723
+// -> 655 us in all, 151936 x 1536 with 187 rows 497 -> 469, with 400 684 -> 668, but with 613 770 either way)
+// (one row of tiles of grad_hidden: 128 x 256 and three stages, 64 rows x 152064 x 3584 715 -> 690 us in all)
+constexpr HeadTile head_tile_hidden(int M) { return M <= 128 ? HeadTile{128, 256} : M <= 256 ? HeadTile{128, 128} : HeadTile{256, 256}; }
+constexpr HeadTile head_tile_head(int K) { return K <= 512 ? HeadTile{128, 128} : HeadTile{256, 256}; }
 
 // Cuts of K for `tiles` tiles of a product with k_tiles slices: rounds over the card's places for workgroups, in slices.  A cut
-// costs the tile's partial results, written and read again, as much as some twenty slices of the largest tile.
+// costs the tile's partial results, written and read again, as much as some twenty slices of a tile that fills a CU.
 constexpr int head_splits(int tiles, int k_tiles, HeadTile t) {
-  const int places = t.m == 256 ? 256 : 512, cost = t.m == 256 ? 20 : 8;
+  const int places = t.n == 256 ? 256 : 512, cost = t.n == 256 ? 20 : 8;
   int best = 1, best_time = head_ceil(tiles, places) * (k_tiles + cost);
   for (int rounds = 1; rounds <= 4; ++rounds) {
     const int s = head_min(places * rounds / tiles, k_tiles / 8);

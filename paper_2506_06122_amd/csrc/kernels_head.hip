@@ -37,6 +37,7 @@ struct Product {
   int M, N, K;            // b with K outermost has exactly K steps; anything else is padded to whole slices
   const HeadActive* plan; // device: TO_GRAD's M, TO_PLANE's M and cuts of K, TO_BF16's K
   HeadGrid grid;
+  bool stream_b;          // STREAM
   void* out;
   long long out_pitch;
   int room;               // rows of the panels that the gradients of logits lie in: TO_GRAD's result, the next products' A
@@ -54,6 +55,11 @@ struct Product {
 
 __device__ __forceinline__ void load_to_lds(unsigned lds, unsigned voff, const void* base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base)
+               : "memory");
+}
+// past the caches
+__device__ __forceinline__ void load_to_lds_once(unsigned lds, unsigned voff, const void* base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(voff), "s"(base)
                : "memory");
 }
 // this wavefront's loads but the last N have arrived and its LDS reads are done; then the barrier
@@ -102,7 +108,9 @@ __device__ __forceinline__ u32x4 fragment(const char* slice, int i, int half, in
 // in registers, so that its buffer takes the copies of stage s + S, and that stage s + 1 has arrived (loads are counted
 // in order, later stages stay in flight), whose first half is read while the second is multiplied.  The copies past the
 // end of K repeat the last slice, so that every stage counts the same number of them.
-template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
+// STREAM: past the caches goes a B that one row of tiles reads, once, and that is larger than the last cache (16 rows x
+// 152064 x 3584 209 -> 191 us; the gradients' products 704 -> 654, 64 rows 779 -> 733).
+template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK, bool STREAM>
 __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void head_product_kernel(Product p) {
   constexpr bool WIDE = MT * NT >= 32;
   constexpr int NW = WM * WN, BM = WM * MT * 16, BN = WN * NT * 16;
@@ -166,7 +174,8 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
     auto issue = [&](int s, int buf) __attribute__((always_inline)) {
       const unsigned to = __builtin_amdgcn_readfirstlane(lds0 + buf * STAGE + dst[s]);
       const unsigned from = BK && ahead == k_tiles - 1 ? tail[s] : voff[s];
-      load_to_lds(to, from, is_b[s] ? pb : pa);
+      if (STREAM && is_b[s]) load_to_lds_once(to, from, pb);
+      else load_to_lds(to, from, is_b[s] ? pb : pa);
     };
     auto move_on = [&]() __attribute__((always_inline)) {
       if (ahead + 1 < kt_end) {
@@ -361,7 +370,8 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
       for (int q = 0; q < MT * 16; q += ROWS) {
         const int ml = q + lane / LANES, m = m0 + wm * MT * 16 + ml;
         const u32x4 w = *(const u32x4*)(mine + ml * OUT_ROW + lane % LANES * 16);
-        if (m < x.m_end && n < n_end) *(u32x4*)(out + m * out_pitch) = w;
+        // past the caches, which the operands need (all three products: 7 rows 404 -> 324 us, 613 rows 832 -> 783, 151936 x 1536)
+        if (m < x.m_end && n < n_end) __builtin_nontemporal_store(w, (u32x4*)(out + m * out_pitch));
       }
       out += rows * out_pitch;
     }
@@ -454,23 +464,31 @@ __global__ __launch_bounds__(256) void head_planes_kernel(const float* part_rows
 template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
 void launch_shape(Product p, int blocks, hipStream_t s) {
   p.grid = head_grid(head_ceil(TO == TO_GRAD ? p.row_capacity : p.M, WM * MT * 16), head_ceil(p.N, WN * NT * 16), 1);
-  head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK><<<blocks ? blocks : head_blocks(p.grid), WM * WN * 64, 0, s>>>(p);
+  const int grid = blocks ? blocks : head_blocks(p.grid);
+  if constexpr (WM == 1) {
+    if (p.stream_b) return head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK, true><<<grid, WM * WN * 64, 0, s>>>(p);
+  }
+  head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK, false><<<grid, WM * WN * 64, 0, s>>>(p);
 }
 static_assert(kHeadTwoPlanes <= 256, "two planes leave tiles of up to 128 rows");
 template <int TO, bool AK, bool BK>
 void launch_product(const Product& p, HeadTile t, int blocks, hipStream_t s) {
   if (t.m == 256) return launch_shape<2, 2, 8, 8, 2, TO, AK, BK>(p, blocks, s);
-  if (t.m == 128) return launch_shape<2, 2, 4, 4, 2, TO, AK, BK>(p, blocks, s);
+  if (t.m == 128 && t.n == 128) return launch_shape<2, 2, 4, 4, TO == TO_SUMS ? 3 : 2, TO, AK, BK>(p, blocks, s);
   if constexpr (TO == TO_SUMS) {
     if (t.m == 160) return launch_shape<2, 2, 5, 8, 2, TO, AK, BK>(p, blocks, s);
     if (t.m == 192) return launch_shape<2, 2, 6, 8, 2, TO, AK, BK>(p, blocks, s);
     if (t.m == 224) return launch_shape<2, 2, 7, 8, 2, TO, AK, BK>(p, blocks, s);
   }
-  if constexpr (!BK) {  // products that walk over W by its rows
-    if (t.m == 64) return launch_shape<1, 4, 4, 4, 2, TO, AK, BK>(p, blocks, s);
+  // one row of tiles: three stages in flight in one workgroup per CU (two stages and two workgroups: x 152064 x 3584, 16
+  // rows 236 -> 211 us, 32 rows 224 -> 192, 64 rows 229 -> 201)
+  if constexpr (!AK) {
+    if (t.m == 128) return launch_shape<1, 4, 8, 4, 3, TO, AK, BK>(p, blocks, s);
+  }
+  if constexpr (!BK) {
+    if (t.m == 64) return launch_shape<1, 4, 4, 4, 3, TO, AK, BK>(p, blocks, s);
     if constexpr (TO == TO_SUMS) {
-      if (t.m == 32) return launch_shape<1, 4, 2, 4, 2, TO, AK, BK>(p, blocks, s);
-      // three stages in flight in one workgroup per CU, 16 x 152064 x 3584 211 us; two stages and two workgroups 236
+      if (t.m == 32) return launch_shape<1, 4, 2, 4, 3, TO, AK, BK>(p, blocks, s);
       return launch_shape<1, 4, 1, 4, 3, TO, AK, BK>(p, blocks, s);
     }
   }
@@ -492,6 +510,7 @@ void launch_head_logprobs(const HeadArgs& in, const TokenOut& out, void* ws, hip
   p.M = in.rows;
   p.N = in.vocab;
   p.K = in.hidden;
+  p.stream_b = in.rows <= 128 && (long long)in.vocab * in.hidden * 2 > kLastCache;
   p.inv_temp = in.inv_temp;
   p.targets = in.targets;
   p.target_logit = (float*)ws;
@@ -535,6 +554,7 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
       p.M = in.rows;
       p.N = v;
       p.K = in.hidden;
+      p.stream_b = room <= 128 && (long long)v * in.hidden * 2 > kLastCache;
       p.plan = plan;
       p.out = dx;
       p.room = (int)room;
@@ -557,6 +577,7 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
       q.M = (int)room;
       q.N = in.hidden;
       q.K = v;
+      q.stream_b = p.stream_b;
       q.plan = plan;
       q.out = part_rows;
       q.out_pitch = in.hidden;

@@ -92,6 +92,7 @@ static void by_tile(const Product& p) {
   if (t.m == 16 && t.n == 256) walk<16, 256, AK, BK>(p);
   else if (t.m == 32 && t.n == 256) walk<32, 256, AK, BK>(p);
   else if (t.m == 64 && t.n == 256) walk<64, 256, AK, BK>(p);
+  else if (t.m == 128 && t.n == 256 && !AK) walk<128, 256, AK, BK>(p);
   else if (t.m == 128 && t.n == 128) walk<128, 128, AK, BK>(p);
   else if (t.m == 160 && t.n == 256 && !AK && !BK) walk<160, 256, AK, BK>(p);
   else if (t.m == 192 && t.n == 256 && !AK && !BK) walk<192, 256, AK, BK>(p);

@@ -102,25 +102,35 @@ def test_sizes(rows, vocab, hidden, entropy):
     check(h, w, t, 0.7 if entropy else 1.0, rows, entropy)
 
 
-def test_tiles_of_every_size_agree_with_the_logits_path():
-    """Large enough for the largest tiles, checked against float64 products on the GPU and the logits' own operator."""
-    import torch
+def agree_with_the_logits_path(h, w, t):
+    """Against float64 products on the GPU and the logits' own operator."""
     import paper_2506_06122_amd as R
+    rows, hidden = h.shape
+    g, e = map(cuda, grads_of(rows, 5, True))
+    x = h.double() @ w.double().T
+    got = R.rollout_head_logprobs(h, w, cuda(t))
+    ref = R.rollout_token_logprobs(x.float(), cuda(t))
+    fuzz = hidden * U * float((h.double().abs() @ w.double().abs().T).max())
+    for a, b in zip(got, ref):
+        assert float((a - b).abs().max()) <= 5 * fuzz + 200 * U * 20
+    dh, dw = R.rollout_head_logprobs_grad(h, w, cuda(t), got[2], got[1], g, e)
+    dx = R.rollout_token_logprobs_grad(x.float(), cuda(t), ref[2], ref[1], g, e).double()
+    for a, b in ((dh, dx @ w.double()), (dw, dx.T @ h.double())):
+        # two roundings to bf16, each at most 2^-8 relative to its value: their norms add up to less than 2^-7
+        assert float((a.double() - b).norm() / b.norm()) <= 2 * BF
+
+
+def test_tiles_of_every_size_agree_with_the_logits_path():
+    """Large enough for the largest tiles."""
     for rows, vocab, hidden in ((1500, 12301, 192), (4096, 4099, 64), (513, 30001, 1536), (150, 50257, 128), (190, 50257, 64),
-                                (310, 32001, 128), (430, 50257, 64)):
-        h, w, t = inputs(rows, vocab, hidden, 5)
-        g, e = map(cuda, grads_of(rows, 5, True))
-        x = h.double() @ w.double().T
-        got = R.rollout_head_logprobs(h, w, cuda(t))
-        ref = R.rollout_token_logprobs(x.float(), cuda(t))
-        fuzz = hidden * U * float((h.double().abs() @ w.double().abs().T).max())
-        for a, b in zip(got, ref):
-            assert float((a - b).abs().max()) <= 5 * fuzz + 200 * U * 20
-        dh, dw = R.rollout_head_logprobs_grad(h, w, cuda(t), got[2], got[1], g, e)
-        dx = R.rollout_token_logprobs_grad(x.float(), cuda(t), ref[2], ref[1], g, e).double()
-        for a, b in ((dh, dx @ w.double()), (dw, dx.T @ h.double())):
-            # two roundings to bf16, each at most 2^-8 relative to its value: their norms add up to less than 2^-7
-            assert float((a.double() - b).norm() / b.norm()) <= 2 * BF
+                                (310, 32001, 128), (430, 50257, 64), (128, 50257, 192), (65, 50257, 64), (420, 12301, 512)):
+        agree_with_the_logits_path(*inputs(rows, vocab, hidden, 5))
+
+
+def test_few_rows_of_an_lm_head_past_the_last_cache():
+    h, w, t = inputs(128, 70001, 2048, 6)  # 287 MB
+    for rows in (1, 9, 16, 20, 32, 50, 64, 100, 128):
+        agree_with_the_logits_path(h[:rows], w, t[:rows])
 
 
 def test_rows_without_gradient_and_no_rows():
