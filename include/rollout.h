@@ -365,6 +365,8 @@ int rollout_policy_loss(int32_t n_seqs, const int32_t *cu_seqlens, const float *
  *     afterwards.  Calls and graphs that may run at the same time need one each.
  *   - dtype: ROLLOUT_DTYPE_F32, _BF16 or _F16.  Strides count elements between rows; inside a row values are consecutive.
  *     Rows need only be aligned to their elements (rollout_head_*: to 16 bytes).
+ *   - Sizes: rows and n up to 2^24 - 64, vocab up to 2^24, hidden up to 2^20; n or rows x hidden up to 2^38; rows x vocab of
+ *     rollout_head_* up to 2^42.
  *   - Sums are fp32, taken in an order that the sizes fix: the same inputs give the same bits.
  *   - Errors: E_INVAL, E_HIP; rollout_last_error(NULL) gives the text. */
 

@@ -17,6 +17,10 @@ void check_sizes(int rows, int vocab, int hidden) {
   if (vocab < 1 || vocab > kMaxVocab) fail(ROLLOUT_E_INVAL, "vocab must be within 1 .. 2^24");
   if (hidden < 1 || hidden > kMaxHidden) fail(ROLLOUT_E_INVAL, "hidden must be within 1 .. 2^20");
 }
+// launches of a workgroup to a row count their threads in 32 bits
+void check_row_launch(int rows) {
+  if (rows > kMaxRows - 64) fail(ROLLOUT_E_INVAL, "rows must not exceed 2^24 - 64");
+}
 // what the launches count in 32 bits
 void check_product(int rows, int hidden) {
   if ((int64_t)rows * hidden > (int64_t)1 << 38) fail(ROLLOUT_E_INVAL, "rows x hidden must not exceed 2^38");
@@ -35,9 +39,9 @@ void check_array(const void* p, size_t align, const char* name) {
 void check_optional(const void* p, size_t align, const char* name) {
   if (p) check_array(p, align, name);
 }
-constexpr int64_t kMaxStride = (int64_t)1 << 40;
+constexpr int64_t kMaxStride = (int64_t)1 << 36;
 void check_stride(int64_t stride, int width, const char* name) {
-  if (stride < width || stride > kMaxStride) fail(ROLLOUT_E_INVAL, std::string(name) + " must be at least the row's length");
+  if (stride < width || stride > kMaxStride) fail(ROLLOUT_E_INVAL, std::string(name) + " must be from the row's length to 2^36");
 }
 // operands of matrix products: 256 rows are reached by a 32-bit offset in bytes
 void check_operand_stride(int64_t stride, int width, const char* name) {
@@ -109,6 +113,7 @@ HeadArgs head_args(const void* hidden_states, int64_t hidden_stride, const void*
   if (hidden % 64) fail(ROLLOUT_E_INVAL, "hidden must be a multiple of 64");
   check_product(rows, hidden);
   check_tiles(rows, vocab);
+  check_row_launch(rows);
   check_operand_stride(hidden_stride, hidden, "hidden_stride");
   check_operand_stride(head_stride, hidden, "head_stride");
   check_optional(targets, 4, "targets");
@@ -124,6 +129,7 @@ extern "C" {
 int64_t rollout_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t top) {
   return bytes_of([&] {
     check_sizes(rows, vocab, 1);
+    check_row_launch(rows);
     check_top(top, vocab);
     return token_workspace(rows, vocab, top);
   });
@@ -135,6 +141,7 @@ int rollout_token_logprobs(const void* logits, int32_t dtype, int32_t rows, int3
                            int32_t* top_ids, float* top_logp) {
   return guarded(nullptr, [&] {
     check_sizes(rows, vocab, 1);
+    check_row_launch(rows);
     check_dtype(dtype);
     check_top(top, vocab);
     check_stride(row_stride, vocab, "row_stride");
@@ -162,6 +169,7 @@ int rollout_token_logprobs_grad(const void* logits, int32_t dtype, int32_t rows,
                                 int64_t grad_row_stride) {
   return guarded(nullptr, [&] {
     check_sizes(rows, vocab, 1);
+    check_row_launch(rows);
     check_dtype(dtype);
     check_stride(row_stride, vocab, "row_stride");
     check_stride(grad_row_stride, vocab, "grad_row_stride");
@@ -237,6 +245,7 @@ int64_t rollout_head_logprobs_workspace(int32_t rows, int32_t vocab, int32_t hid
     check_sizes(rows, vocab, hidden);
     check_product(rows, hidden);
     check_tiles(rows, vocab);
+    check_row_launch(rows);
     return head_workspace(rows, vocab, hidden);
   });
 }
@@ -262,6 +271,7 @@ int64_t rollout_head_logprobs_grad_workspace(int32_t rows, int32_t vocab, int32_
     check_sizes(rows, vocab, hidden);
     check_product(rows, hidden);
     check_tiles(rows, vocab);
+    check_row_launch(rows);
     return head_grad_workspace(rows, vocab, hidden);
   });
 }

@@ -19,7 +19,7 @@ namespace {
 template <typename V, bool VEC, bool STREAM>
 __global__ __launch_bounds__(256) void embed_rows_kernel(EmbedArgs a, int per_row) {
   constexpr int E = VEC ? kVec<V> : 1;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long at = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
   const long long r = at / per_row;
   if (r >= a.n) return;
   const int col = (int)(at - r * per_row) * E;
@@ -51,7 +51,7 @@ void launch_rows(const EmbedArgs& a, hipStream_t s) {
   constexpr int E = kVec<V>;
   const bool vec = a.hidden % E == 0 && a.table_stride % E == 0 && (((size_t)a.table | (size_t)a.out) & 15) == 0;
   const int per_row = vec ? a.hidden / E : a.hidden;
-  const int grid = ceil_div((long long)a.n * per_row, 256);
+  const dim3 grid = many_blocks(((long long)a.n * per_row + 255) / 256);
   const bool stream = (long long)a.n * a.hidden * sizeof(V) > kLastCache / 4;
   if (vec && stream) embed_rows_kernel<V, true, true><<<grid, 256, 0, s>>>(a, per_row);
   else if (vec) embed_rows_kernel<V, true, false><<<grid, 256, 0, s>>>(a, per_row);

@@ -130,7 +130,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
   const int pad = TO == TO_GRAD ? head_pad(p.planes) : 0, rows = TO == TO_GRAD ? head_up(M, pad) : M;
   if constexpr (TO == TO_GRAD || TO == TO_PLANE) grid = head_grid_rows(grid, head_ceil(rows, BM));
   if constexpr (TO == TO_PLANE) grid.splits = p.plan->splits;
-  const HeadBlock block = head_block(blockIdx.x, grid);
+  const HeadBlock block = head_block(blockIdx.y * gridDim.x + blockIdx.x, grid);
   if (!block.inside) return;
   const int bn = block.n, bz = block.z;
   const int m0 = block.m * BM, n0 = bn * BN;
@@ -435,7 +435,7 @@ __global__ __launch_bounds__(256) void head_planes_kernel(const float* part_rows
   __shared__ f32x4 part[3][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per_row = hidden / 4;
-  const long long at = (long long)blockIdx.x * 64 + lane;
+  const long long at = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 64 + lane;
   const int row = (int)min(at / per_row, (long long)rows - 1), col = (int)(at % per_row) * 4;
   const int stacked = plan->stacked, second = planes == 2 ? stacked / 2 : 0;
   const int i = place[row], splits = plan->splits, share = (splits + 3) / 4, end = min(splits, (wave + 1) * share);
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(256) void head_planes_kernel(const float* part_rows
 template <int WM, int WN, int MT, int NT, int S, int TO, bool AK, bool BK>
 void launch_shape(Product p, int blocks, hipStream_t s) {
   p.grid = head_grid(head_ceil(TO == TO_GRAD ? p.row_capacity : p.M, WM * MT * 16), head_ceil(p.N, WN * NT * 16), 1);
-  const int grid = blocks ? blocks : head_blocks(p.grid);
+  const dim3 grid = many_blocks(blocks ? blocks : head_blocks(p.grid));
   if constexpr (WM == 1) {
     if (p.stream_b) return head_product_kernel<WM, WN, MT, NT, S, TO, AK, BK, true><<<grid, WM * WN * 64, 0, s>>>(p);
   }
@@ -596,6 +596,6 @@ void launch_head_logprobs_grad(const HeadGrad& a, void* ws, hipStream_t s) {
     launch_product<TO_BF16, true, true>(q, head_tile_head(in.rows), 0, s);
   }
   if (in.rows > 0)
-    head_planes_kernel<<<ceil_div((long long)in.rows * (in.hidden / 4), 64), 256, 0, s>>>(part_rows, g.planes, plan, in.rows, in.hidden, place,
-                                                                                   (uint16_t*)a.grad_hidden);
+    head_planes_kernel<<<many_blocks(((long long)in.rows * (in.hidden / 4) + 63) / 64), 256, 0, s>>>(part_rows, g.planes, plan, in.rows, in.hidden,
+                                                                                              place, (uint16_t*)a.grad_hidden);
 }

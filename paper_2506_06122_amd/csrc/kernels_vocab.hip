@@ -121,8 +121,8 @@ __device__ void top_of_slice(const RowSlice<V>& row, int runs, int steps, int K,
   const int one = row.single(tid);
   if (one >= 0) consider(to_f32(row.x[one]), one);
   __syncthreads();
-  // vector w of the runs to read: step w % steps of run hot[w / steps]; the quotient by a product is exact, since
-  // w + 1/2 is at least 1 / (2 steps) of it away from a whole number and w < 2^20
+  // vector w of the runs to read: step w % steps of run hot[w / steps]; the quotient by a product is at most one off, in
+  // rows of millions of values, and the remainder tells
   const int n_vecs = sh.n_hot * steps;
   const float by = 1.0f / (float)steps;
   for (int w0 = tid; w0 < n_vecs; w0 += U * T) {
@@ -130,7 +130,8 @@ __device__ void top_of_slice(const RowSlice<V>& row, int runs, int steps, int K,
     int at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int w = w0 + u * T, h = min((int)(((float)w + 0.5f) * by), sh.n_hot - 1), hot = sh.hot[h];
+      const int w = w0 + u * T, about = (int)(((float)w + 0.5f) * by), over = w - about * steps;
+      const int h = about + (over >= steps) - (over < 0), hot = sh.hot[min(h, sh.n_hot - 1)];
       at[u] = row.begin + ((hot / T) * steps + w - h * steps) * T + hot % T;
       if (w >= n_vecs || at[u] >= row.end) at[u] = -1;
       else v4[u] = row.vec(at[u]);
@@ -399,9 +400,9 @@ void launch_grad(const TokenGrad& a, hipStream_t s) {
   const size_t size = sizeof(V);
   const bool same = (((size_t)a.in.logits - (size_t)a.out) & 15) == 0 && ((a.in.stride - a.out_stride) * size & 15) == 0;
   const bool stream = (long long)a.in.rows * a.in.vocab * size > kLastCache;
-  // a vector to a thread, as long as the workgroups can be counted
+  // a vector to a thread, as long as 32 bits count the threads
   int parts = std::max(1, ceil_div(a.in.vocab, T * kVec<V>));
-  while ((long long)a.in.rows * parts > 0x7fffffff) parts = (parts + 1) / 2;
+  while (parts > 1 && (long long)a.in.rows * parts > 0xffffff) parts = (parts + 1) / 2;
   const int grid = a.in.rows * parts;
   if (same && stream) token_grad_kernel<V, true, true><<<grid, T, 0, s>>>(a, parts);
   else if (same) token_grad_kernel<V, true, false><<<grid, T, 0, s>>>(a, parts);

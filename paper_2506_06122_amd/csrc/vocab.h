@@ -10,6 +10,13 @@ constexpr size_t vt_size(int dtype) { return dtype == VT_F32 ? 4 : 2; }
 
 constexpr long long kLastCache = 256ll << 20;  // bytes of the cache before memory
 
+// Workgroups of 256 threads: a launch counts the threads along x in 32 bits, so that more than 2^23 workgroups go into rows
+// of the grid.  The last row may reach past `blocks`.
+inline dim3 many_blocks(long long blocks) {
+  const long long x = 1ll << 23;
+  return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+
 constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
 
 // ---- logits ------------------------------------------------------------------------------

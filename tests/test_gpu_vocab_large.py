@@ -1,0 +1,101 @@
+"""The operators at the vocabulary's ends where launches have more than 2^32 threads or rows are the longest that there are.
+Tens of GB each, made on the GPU."""
+import pytest
+
+U, BF = 2.0 ** -24, 2.0 ** -8
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def memory():
+    import torch
+    if torch.cuda.get_device_properties(0).total_memory < 120 << 30:
+        pytest.skip("needs 120 GB of GPU memory")
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_the_most_rows_of_logits():
+    import torch
+    import paper_2506_06122_amd as R
+    torch.manual_seed(1)
+    rows = (1 << 24) - 64
+    x = torch.randn(rows, 5, device="cuda").bfloat16()
+    t = torch.randint(0, 5, (rows,), device="cuda", dtype=torch.int32)
+    g = torch.randn(rows, device="cuda")
+    logp, ent, stats, ids, _ = R.rollout_token_logprobs(x, t, top=1)
+    lp = torch.log_softmax(x.double(), 1)
+    # |x - max| < 13: ln S is off by its exponents' (2 x 18 + 8) U, the difference by 2 x 13 U, the logarithm by a few
+    assert float((logp - lp.gather(1, t.long()[:, None])[:, 0]).abs().max()) <= 80 * U
+    assert bool((x.gather(1, ids.long()) == x.max(1, keepdim=True).values).all())
+    got = R.rollout_token_logprobs_grad(x, t, stats, ent, g)
+    want = -lp.exp() * g[:, None]
+    want.scatter_add_(1, t.long()[:, None], g[:, None].double())
+    off = (got - want).abs() - BF * want.abs() - 100 * U * g.abs()[:, None]
+    assert float(off.max()) <= 0
+
+
+def test_many_odd_rows_of_an_embedding():
+    import torch
+    import paper_2506_06122_amd as R
+    torch.manual_seed(2)
+    n, hidden = (1 << 20) + 3, 4100  # a value to a thread: past 2^32 threads
+    table = torch.randn(11, hidden, device="cuda").bfloat16()
+    tokens = torch.randint(-1, 11, (n,), device="cuda", dtype=torch.int32)
+    out = R.rollout_embed(table, tokens)
+    rows = torch.cat([table, torch.zeros(1, hidden, device="cuda").bfloat16()])  # -1: the last
+    for i in range(0, n, 1 << 17):
+        assert torch.equal(out[i:i + (1 << 17)], rows[tokens[i:i + (1 << 17)].long()])
+
+
+def test_head_gradients_of_many_states():
+    import torch
+    import paper_2506_06122_amd as R
+    torch.manual_seed(3)
+    rows, vocab, hidden = (1 << 20) + 5, 256, 4096
+    h = torch.empty(rows, hidden, device="cuda", dtype=torch.bfloat16).normal_()
+    w = (torch.randn(vocab, hidden, device="cuda") / 64).bfloat16()
+    t = torch.randint(0, vocab, (rows,), device="cuda", dtype=torch.int32)
+    g = torch.randn(rows, device="cuda")
+    g[::3] = 0
+    logp, ent, stats = R.rollout_head_logprobs(h, w, t)
+    dh, dw = R.rollout_head_logprobs_grad(h, w, t, stats, ent, g)
+    assert not dh[::3].any()
+    for at in (0, rows // 2, rows - 500):
+        s = slice(at, at + 500)
+        p = torch.softmax(h[s].double() @ w.double().T, 1)
+        d = -p * g[s, None]
+        d.scatter_add_(1, t[s].long()[:, None], g[s, None].double())
+        want = d @ w.double()
+        # two roundings to bf16, each at most 2^-8 relative to its value: their norms add up to less than 2^-7
+        assert float((dh[s].double() - want).norm() / want.norm()) <= 2 * BF
+    total = torch.zeros(vocab, hidden, device="cuda", dtype=torch.float64)
+    for at in range(0, rows, 1 << 17):
+        s = slice(at, at + (1 << 17))
+        p = torch.softmax(h[s].double() @ w.double().T, 1)
+        d = -p * g[s, None]
+        d.scatter_add_(1, t[s].long()[:, None], g[s, None].double())
+        total += d.T.contiguous() @ h[s].double()
+    assert float((dw.double() - total).norm() / total.norm()) <= 2 * BF
+
+
+def test_equal_greatest_values_in_the_longest_rows():
+    """One greatest value in each of a workgroup's 4 x 256 runs of vectors, at either end of it."""
+    import torch
+    import paper_2506_06122_amd as R
+    rows, vocab = 1024, 1 << 24
+    steps = vocab // 8 // 1024
+    x = torch.zeros(rows, vocab, device="cuda", dtype=torch.bfloat16)
+    run, thread = torch.meshgrid(torch.arange(4), torch.arange(256), indexing="ij")
+    step = torch.where((run + thread) % 2 == 0, 0, steps - 1)
+    where = (((run * steps + step) * 256 + thread) * 8 + thread % 8).flatten()
+    x.index_fill_(1, where.cuda(), 1.0)
+    logp, ent, stats, ids, alt = R.rollout_token_logprobs(x, top=64)
+    first = where.sort().values[:64].int().cuda()
+    assert bool((ids == first).all())
+    # ln(1024 e + (2^24 - 1024)) - 1, summed in 2^11 or so steps a thread and then joined
+    import math
+    log_s = math.log(1024 + (vocab - 1024) / math.e)
+    assert float((stats[:, 1].double() - log_s).abs().max()) <= (vocab // 256) * U
+    assert float((alt.double() + log_s).abs().max()) <= (vocab // 256) * U
