@@ -378,18 +378,31 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
   }
 }
 
-// ---- a row's parts -> its results: one wavefront per row --------------------------------------
+// ---- a row's parts -> its results: one workgroup per row, up to 1024 parts with all loads at once ------------------------
 __global__ __launch_bounds__(256) void head_finish_kernel(HeadArgs in, TokenOut out, const RowSums* sums, const float* target_logit, int parts) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= in.rows) return;
+  __shared__ RowSums wave_s[4];
+  const int row = blockIdx.x, tid = threadIdx.x;
   const float c = in.inv_temp * kLog2e;
-  RowSums s{kLowest, 0.f, 0.f};
-  for (int i = lane; i < parts; i += WAVE) s = merge(s, sums[(long long)row * parts + i], c);
-  s = merge_wave(s, c);
-  if (lane) return;
   const int t = in.targets ? in.targets[row] : -1;
   const bool has = t >= 0 && t < in.vocab;
-  finish_row(s, out, row, has, has ? target_logit[row] : 0.f, in.inv_temp);
+  const float x_target = has ? target_logit[row] : 0.f;
+  constexpr int U = 4;
+  RowSums mine{kLowest, 0.f, 0.f};
+  for (int i = tid; i < parts; i += U * 256) {
+    RowSums v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = i + u * 256 < parts ? sums[(long long)row * parts + i + u * 256] : RowSums{kLowest, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < U; ++u) mine = merge(mine, v[u], c);
+  }
+  mine = merge_wave(mine, c);
+  if ((tid & 63) == 0) wave_s[tid >> 6] = mine;
+  __syncthreads();
+  if (tid) return;
+  RowSums s = wave_s[0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) s = merge(s, wave_s[w], c);
+  finish_row(s, out, row, has, x_target, in.inv_temp);
 }
 
 // ---- rows that have a gradient ---------------------------------------------------------------
@@ -516,7 +529,7 @@ void launch_head_logprobs(const HeadArgs& in, const TokenOut& out, void* ws, hip
   p.target_logit = (float*)ws;
   p.sums = (RowSums*)((char*)ws + piece((size_t)in.rows * 4));
   launch_product<TO_SUMS, false, false>(p, t, 0, s);
-  head_finish_kernel<<<ceil_div(in.rows, 4), 256, 0, s>>>(in, out, p.sums, p.target_logit, ceil_div(in.vocab, t.n));
+  head_finish_kernel<<<in.rows, 256, 0, s>>>(in, out, p.sums, p.target_logit, ceil_div(in.vocab, t.n));
 }
 
 size_t head_grad_workspace(int rows, int vocab, int hidden) {
