@@ -7,6 +7,9 @@
 // of equal ids in fp32, in the order of the rows, so the result does not depend on scheduling.  It takes a chunk of sorted
 // rows to a workgroup whatever the ids are: a run that crosses the edge of a chunk leaves partial sums, and the third
 // launch joins those in order.
+//
+// Lookup of 16384 rows x 3584 bf16: 34.5 us, 6.8 TB/s of results and rows that the caches hold in part.  Gradient of as many
+// rows, 152064 ids: 184 us of sorting and filling (5.9 TB/s), 35 of sums, 8 of joins.
 #include "vocab.h"
 #include "vocab_vec.h"
 
@@ -52,7 +55,9 @@ void launch_rows(const EmbedArgs& a, hipStream_t s) {
   const bool vec = a.hidden % E == 0 && a.table_stride % E == 0 && (((size_t)a.table | (size_t)a.out) & 15) == 0;
   const int per_row = vec ? a.hidden / E : a.hidden;
   const dim3 grid = many_blocks(((long long)a.n * per_row + 255) / 256);
-  const bool stream = (long long)a.n * a.hidden * sizeof(V) > kLastCache / 4;
+  // results larger than the XCDs' own caches go past them (x 3584 bf16, us past / through: 1024 rows 7.03 / 7.02, 4096 rows
+  // 8.6 / 10.5, 16384 rows 34.5 / 43.5)
+  const bool stream = (long long)a.n * a.hidden * sizeof(V) > 16 << 20;
   if (vec && stream) embed_rows_kernel<V, true, true><<<grid, 256, 0, s>>>(a, per_row);
   else if (vec) embed_rows_kernel<V, true, false><<<grid, 256, 0, s>>>(a, per_row);
   else embed_rows_kernel<V, false, false><<<grid, 256, 0, s>>>(a, per_row);
@@ -62,7 +67,8 @@ void launch_rows(const EmbedArgs& a, hipStream_t s) {
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / WAVE;
 constexpr int kRange = 512;   // ids of a sorting workgroup at most: kSortWaves counters each are 32 KB of LDS
 // sorted rows of a summing workgroup: as many rows as fill the card, each workgroup with a few in flight; with many rows more,
-// since each chunk may leave two rows of partial sums
+// since each chunk may leave two rows of partial sums (152064 x 3584 bf16 on top of a base, us with 4 / 16: 1021 rows 14.5 / 17.8,
+// 4096 rows 26.2 / 27.8, 8192 rows 43.0 / 40.3)
 constexpr int chunk_rows(int n) { return n <= 4096 ? 4 : 16; }
 constexpr int kFill = 8192;   // 16-byte vectors of the matrix that a filling workgroup writes
 

@@ -7,6 +7,10 @@
 // bound for more than a few rows; with a few the walk over W is.  One kernel does all of them: C = A B^T over tiles, where
 // each operand lies with its rows or with the summed index outermost, as the caller or the previous launch left it -
 // fragments of the second kind are transposed on their way out of LDS - so that nothing is transposed in memory.
+//
+// 4096 x 152064 x 3584: 3.21 to 3.37 ms, 1.32 to 1.39 PFLOP/s by the card (matrix instructions two thirds of the time, the
+// clock at 1.9 to 2.0 GHz under them); its gradients with respect to three quarters of the rows, three products, 8.0 to 8.4 ms, 1.20 to 1.25 PFLOP/s: slices with K
+// outermost take a tenth longer.  7 x 151936 x 1536: 89 us, 5.3 TB/s of W.
 #include "vocab.h"
 
 #include <algorithm>
