@@ -155,3 +155,14 @@ def test_streams_and_graphs():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
+def test_the_null_stream_by_its_handle():
+    import torch
+    import paper_2506_06122_amd as R
+    ids, table = cuda(ids_of("padded", 70, 100, 4)), torch.randn(100, 48, device="cuda")
+    want = R.rollout_embed(table, ids), R.rollout_embed_grad(table[:70], ids, 100)
+    torch.cuda.synchronize()
+    got = R.rollout_embed(table, ids, stream=0), R.rollout_embed_grad(table[:70], ids, 100, stream=0)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
