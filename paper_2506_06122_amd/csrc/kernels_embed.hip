@@ -9,7 +9,7 @@
 // launch joins those in order.
 //
 // Lookup of 16384 rows x 3584 bf16: 34.5 us, 6.8 TB/s of results and rows that the caches hold in part.  Gradient of as many
-// rows, 152064 ids: 184 us of sorting and filling (5.9 TB/s), 35 of sums, 8 of joins.
+// rows, 152064 ids: 175 us of sorting and filling (6.2 TB/s), 35 of sums, 8 of joins.
 #include "vocab.h"
 #include "vocab_vec.h"
 
@@ -70,7 +70,11 @@ constexpr int kRange = 512;   // ids of a sorting workgroup at most: kSortWaves 
 // since each chunk may leave two rows of partial sums (152064 x 3584 bf16 on top of a base, us with 4 / 16: 1021 rows 14.5 / 17.8,
 // 4096 rows 26.2 / 27.8, 8192 rows 43.0 / 40.3)
 constexpr int chunk_rows(int n) { return n <= 4096 ? 4 : 16; }
-constexpr int kFill = 8192;   // 16-byte vectors of the matrix that a filling workgroup writes
+// 16-byte vectors of the matrix that a filling workgroup writes (`filled`): one to a thread where they are many, so that the workgroups that
+// run at a time write neighbouring addresses (whole calls, us by 1 / 8 to a thread: 1021 rows, 152064 x 3584 bf16 184 / 194, with a base in fp32
+// 822 / 860, but 4096 rows, 32001 x 1536 28.8 / 24.5)
+// (past 32 GB again eight: 32 bits count a launch's threads)
+constexpr int fill_vectors(long long bytes) { return bytes > kLastCache && bytes <= 32ll << 30 ? kSortThreads : 8 * kSortThreads; }
 
 struct EmbedSort {
   int* row;        // [n] rows sorted by id, equal ids in the order of the rows
@@ -99,7 +103,7 @@ EmbedPlan plan(int n, int vocab) {
 // walk puts them there: the order within an id is the order of the rows, and no workgroup waits for another.  The
 // workgroups behind them fill the matrix.
 template <typename G>
-__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, EmbedSort q, int ranges, int range, bool fill, bool stream) {
+__global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, EmbedSort q, int ranges, int range, int filled, bool fill, bool large) {
   __shared__ int count_s[kSortWaves][kRange];
   __shared__ int below_s[kSortWaves], scan_s[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -118,15 +122,15 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(EmbedGrad a, E
     u32x4* o = (u32x4*)(out + head);
     const u32x4* b = (const u32x4*)(base + head);
     const u32x4 none = {0, 0, 0, 0};
-    const long long first = block * kFill + tid, end = min(vecs, (block + 1) * (long long)kFill);
+    const long long first = block * filled + tid, end = min(vecs, (block + 1) * (long long)filled);
     // what is larger than the last cache passes it by (152064 x 3584 in bf16, the whole call: 248 -> 232 us)
-    if (!base && stream) {
+    if (!base && large) {
 #pragma unroll 4
       for (long long i = first; i < end; i += kSortThreads) __builtin_nontemporal_store(none, o + i);
     } else if (!base) {
 #pragma unroll 4
       for (long long i = first; i < end; i += kSortThreads) o[i] = none;
-    } else if (stream && (((size_t)base - (size_t)out) & 15) == 0) {
+    } else if (large && (((size_t)base - (size_t)out) & 15) == 0) {
 #pragma unroll 4
       for (long long i = first; i < end; i += kSortThreads) __builtin_nontemporal_store(__builtin_nontemporal_load(b + i), o + i);
     } else if ((((size_t)base - (size_t)out) & 15) == 0) {
@@ -330,8 +334,8 @@ void launch_grad(const EmbedGrad& a, void* ws, hipStream_t s) {
   q.last = (float*)take((size_t)p.chunks * a.hidden * 4);
   const bool fill = a.base != a.out;
   const long long bytes = (long long)a.vocab * a.hidden * sizeof(G);
-  const int fillers = fill ? ceil_div(bytes, kFill * 16) : 0;
-  embed_sort_kernel<G><<<p.ranges + fillers, kSortThreads, 0, s>>>(a, q, p.ranges, p.range, fill, bytes > kLastCache);
+  const int filled = fill_vectors(bytes), fillers = fill ? ceil_div(bytes, filled * 16) : 0;
+  embed_sort_kernel<G><<<p.ranges + fillers, kSortThreads, 0, s>>>(a, q, p.ranges, p.range, filled, fill, bytes > kLastCache);
   if (p.chunks == 0) return;
   // whole vectors of 8 values: every row starts on 16 bytes
   const bool vec = a.hidden % 8 == 0 && a.row_stride % 8 == 0 && (((size_t)a.grad_rows | (size_t)a.base | (size_t)a.out) & 15) == 0;

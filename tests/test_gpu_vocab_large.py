@@ -99,3 +99,24 @@ def test_equal_greatest_values_in_the_longest_rows():
     log_s = math.log(1024 + (vocab - 1024) / math.e)
     assert float((stats[:, 1].double() - log_s).abs().max()) <= (vocab // 256) * U
     assert float((alt.double() + log_s).abs().max()) <= (vocab // 256) * U
+
+
+def test_gradient_of_a_matrix_past_32_gb():
+    import torch
+    import paper_2506_06122_amd as R
+    torch.manual_seed(5)
+    vocab, hidden, n = 1 << 22, 4160, 3000  # 35 GB
+    ids = torch.randint(0, vocab, (n,), device="cuda", dtype=torch.int32)
+    ids[:5] = torch.tensor([vocab - 1, 0, 17, vocab - 1, vocab])
+    dy = torch.randn(n, hidden, device="cuda").bfloat16()
+    out = torch.full((vocab, hidden), 1.0, dtype=torch.bfloat16, device="cuda")
+    R.rollout_embed_grad(dy, ids, vocab, out=out)
+    inside = ids < vocab
+    rows, at = ids[inside].long().unique(return_inverse=True)
+    want = torch.zeros(len(rows), hidden, device="cuda", dtype=torch.float64).index_add_(0, at, dy[inside].double())
+    got = out[rows]
+    # few rows to an id: the sum's roundings are far below half a step of bf16
+    assert float(((got.double() - want).abs() - BF * 1.001 * want.abs()).max()) <= 1e-6
+    out[rows] = 0
+    for i in range(0, vocab, 1 << 19):
+        assert not out[i:i + (1 << 19)].any()
