@@ -13,7 +13,7 @@
 //
 // A row belongs to one workgroup where rows are enough; fewer are cut into parts whose results a second launch joins.
 //
-// 2048 x 152064 bf16: 108 us without alternatives, 5.8 TB/s; 120 us with 8.  A lone row of 151936 fp32 with 20: 7.4 and 6.7 us.
+// 2048 x 152064 bf16: 94 us without alternatives, 6.6 TB/s; 107 us with 8.  A lone row of 151936 fp32 with 20: 7.4 and 6.7 us.
 #include "vocab.h"
 #include "vocab_vec.h"
 
@@ -197,9 +197,12 @@ __device__ inline void store_top(const TokenOut& o, int row, int rank, unsigned 
   o.top_logp[at] = log_s == -INFINITY ? -INFINITY : (key_value((unsigned)(key >> 32)) - m) * inv_temp - log_s;
 }
 
-template <typename V, bool TOP>
+// STREAM: past the caches
+template <typename V, bool TOP, bool STREAM>
 __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOut out, TokenParts p) {
-  constexpr int E = kVec<V>, U = 4;
+  // vectors in flight: eight where nothing else holds registers (x 152064 bf16, 2048 rows 94 us, four 99; but through the caches 300
+  // rows 23.2 and 21.5, with 8 alternatives 2048 rows 129 and 122)
+  constexpr int E = kVec<V>, U = STREAM && !TOP ? 8 : 4;
   __shared__ RowSums wave_s[NW];
   __shared__ float log_s_s;
   __shared__ std::conditional_t<TOP, TopShared, int> sh;
@@ -224,7 +227,7 @@ __global__ __launch_bounds__(T) void token_logprobs_kernel(TokenRows in, TokenOu
       u32x4 w[U];
       float v[U * E];
 #pragma unroll
-      for (int u = 0; u < U; ++u) w[u] = row.vec(i + u * T);
+      for (int u = 0; u < U; ++u) w[u] = STREAM ? __builtin_nontemporal_load((const u32x4*)(row.x + row.id(i + u * T))) : row.vec(i + u * T);
 #pragma unroll
       for (int u = 0; u < U; ++u) widen(w[u], v + u * E, V{});
       top = fmaxf(top, add_chunk<U * E>(sums, v, c));
@@ -392,8 +395,14 @@ TokenParts layout(int rows, int vocab, int top, void* ws) {
 template <typename V>
 void launch(const TokenRows& in, const TokenOut& out, const TokenParts& p, hipStream_t s) {
   const int grid = in.rows * p.parts;
-  if (out.top) token_logprobs_kernel<V, true><<<grid, T, 0, s>>>(in, out, p);
-  else token_logprobs_kernel<V, false><<<grid, T, 0, s>>>(in, out, p);
+  // logits larger than the last cache (x 152064 bf16, us past / through the caches: 2048 rows 99 / 107, 1300 rows with 8
+  // alternatives 85 / 91, 1000 rows 58 / 58)
+  const bool stream = (long long)in.rows * in.vocab * (long long)sizeof(V) > kLastCache;
+  const auto pass = [&](auto top, auto past) {
+    token_logprobs_kernel<V, decltype(top)::value, decltype(past)::value><<<grid, T, 0, s>>>(in, out, p);
+  };
+  const auto by_size = [&](auto top) { stream ? pass(top, std::true_type{}) : pass(top, std::false_type{}); };
+  out.top ? by_size(std::true_type{}) : by_size(std::false_type{});
   if (p.parts == 1) return;
   if (out.top) token_join_kernel<V, true><<<in.rows, T, (size_t)p.parts * out.top * 8, s>>>(in, out, p);
   else token_join_kernel<V, false><<<in.rows, T, 0, s>>>(in, out, p);

@@ -120,3 +120,37 @@ def test_gradient_of_a_matrix_past_32_gb():
     out[rows] = 0
     for i in range(0, vocab, 1 << 19):
         assert not out[i:i + (1 << 19)].any()
+
+
+@pytest.mark.parametrize("vocab,pad", [(152064, 0), (152063, 2)])
+def test_logits_past_the_last_cache(vocab, pad):
+    import math
+    import torch
+    import paper_2506_06122_amd as R
+    torch.manual_seed(6)
+    rows = 1100  # 335 MB
+    buf = torch.empty(rows, vocab + pad, device="cuda", dtype=torch.bfloat16).normal_(0, 3)
+    x = buf[:, pad:]
+    x[7] = -math.inf
+    x[8, 1000:] = -math.inf
+    t = torch.randint(-1, vocab, (rows,), device="cuda", dtype=torch.int32)
+    lp = torch.log_softmax(x.double(), 1)
+    want = torch.where(t >= 0, lp.gather(1, t.clamp(min=0).long()[:, None])[:, 0], 0.0)
+    ent = -(lp.exp() * lp.clamp(min=-1e9)).sum(1)
+    ent[7] = 0
+    want[7] = -math.inf if int(t[7]) >= 0 else 0.0
+    live = torch.ones(rows, dtype=torch.bool, device="cuda")
+    live[7] = False
+    # sums of vocab / 256 values a thread, the threads' below each other, exponents of up to 2 x 30
+    n = vocab / 256 + 60
+    for top in (0, 5):
+        logp, h, stats, ids, alt = R.rollout_token_logprobs(x, t, top=top)
+        held = live & torch.isfinite(want)
+        assert bool((logp == want)[~held].all())
+        # |logp| <= 40: its two differences round by 4 U of that
+        assert float((logp - want).abs()[held].max()) <= (n + 8) * U + 4 * U * 40
+        assert float((h - ent).abs().max()) <= (3 * n + 40) * U * math.log(vocab + 2)
+        if top:
+            best = x.double().topk(top, 1).values
+            assert bool((x.double().gather(1, ids.long()) == best)[live].all())
+            assert float((alt - (lp.gather(1, ids.long())))[live].abs().max()) <= (n + 8) * U + 4 * U * 40
