@@ -159,3 +159,17 @@ def test_the_binding_takes_gpu_tensors(bad):
         with pytest.raises(R.RolloutError) as e:
             f()
         assert e.value.code == B.E_INVAL
+
+
+@pytest.mark.parametrize("name,args,changed,word", [
+    ("rollout_token_logprobs", TOKENS, dict(rows=(1 << 24) - 63), "2^24 - 64"),
+    ("rollout_token_logprobs_grad", GRAD, dict(rows=(1 << 24) - 63), "2^24 - 64"),
+    ("rollout_head_logprobs", HEAD, dict(rows=(1 << 24) - 63), "2^24 - 64"),
+    ("rollout_head_logprobs_grad", HEAD_GRAD, dict(rows=(1 << 24) - 63), "2^24 - 64"),
+    ("rollout_token_logprobs", TOKENS, dict(row_stride=(1 << 36) + 1), "2^36"),
+    ("rollout_embed", EMBED, dict(table_stride=(1 << 36) + 1), "2^36"),
+    ("rollout_embed_grad", EMBED_GRAD, dict(row_stride=(1 << 36) + 1), "2^36"),
+])
+def test_refused_past_the_limits(name, args, changed, word):
+    rc, text = call(name, args, **changed)
+    assert rc == B.E_INVAL and word in text, (rc, text)
