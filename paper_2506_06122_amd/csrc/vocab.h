@@ -3,6 +3,7 @@
 // lookup and gradient.  All launches are asynchronous on the given stream; every pointer is device memory the caller owns.
 #pragma once
 #include "common.h"
+#include "row_sums.h"
 
 // Element type of a caller's tensor: ROLLOUT_DTYPE_*.
 enum { VT_F32 = 0, VT_BF16 = 1, VT_F16 = 2 };
@@ -17,8 +18,6 @@ inline dim3 many_blocks(long long blocks) {
   return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
 }
 
-constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e430p-1f;
-
 // ---- logits ------------------------------------------------------------------------------
 constexpr int kTopMax = 64;        // alternatives per row
 constexpr int kTokenThreads = 256;
@@ -30,14 +29,6 @@ struct TokenRows {
   float inv_temp;
   const int* targets;  // [rows] or NULL; ids outside [0, vocab): no target
 };
-// What one pass leaves of (a part of) a row: m = the maximum (at least the lowest finite float), and over y = x log2(e) / T - r
-// the sums of 2^y and y 2^y.  The reference r is the maximum's exponent m log2(e) / T rounded to a whole number, so that
-// one fused multiply-add gives y without a rounding of r, and moving to another reference is exact; where that product
-// leaves fp32's range of exponents, y = (x - m) log2(e) / T instead.
-struct RowSums {
-  float m, s, t;
-};
-constexpr float kLowest = -3.402823466e38f;
 struct TokenOut {
   float* logp;       // [rows]
   float* entropy;    // [rows]
@@ -88,55 +79,6 @@ __device__ inline float grad_of(float x, float c, const RowGrad& r) {
   return __builtin_amdgcn_exp2f(y) * fmaf(r.b, fmaxf(y, -1e30f), r.a);
 }
 
-__device__ inline bool plain_exponent(float mc) { return fabsf(mc) < 1e30f; }
-// binary orders of magnitude from the reference of maximum `from` up to that of `to` >= from; past 1e30 it is as good as
-// infinite, and 0 x infinity would be NaN
-__device__ inline float raise(float from, float to, float c) {
-  const float a = from * c, b = to * c;
-  const float d = plain_exponent(a) && plain_exponent(b) ? rintf(b) - rintf(a) : (to - from) * c;
-  return fminf(d, 1e30f);
-}
-__device__ inline RowSums merge(const RowSums& p, const RowSums& q, float c) {
-  const float m = fmaxf(p.m, q.m), dp = raise(p.m, m, c), dq = raise(q.m, m, c);
-  const float fp = __builtin_amdgcn_exp2f(-dp), fq = __builtin_amdgcn_exp2f(-dq);
-  return RowSums{m, p.s * fp + q.s * fq, (p.t - dp * p.s) * fp + (q.t - dq * q.s) * fq};
-}
-// s and t with N more values, none above m.  The quick form makes a NaN of 0 x -inf for values of -inf (and of anything the
-// plain exponent cannot hold): such chunks are summed again with care, and what is NaN or +inf among the values stays NaN.
-template <int N>
-__device__ inline RowSums sum_below(float m, float s0, float t0, const float* v, float c) {
-  const float ref = rintf(m * c);
-  float s = s0, t = t0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float y = fmaf(v[i], c, -ref), e = __builtin_amdgcn_exp2f(y);
-    s += e;
-    t = fmaf(e, y, t);
-  }
-  if (!(fabsf(t) < 1e30f)) {
-    s = s0;
-    t = t0;
-    const bool plain = plain_exponent(m * c);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float y = plain ? fmaf(v[i], c, -ref) : (v[i] - m) * c, e = __builtin_amdgcn_exp2f(y);
-      s += e;
-      t = fmaf(e, fmaxf(y, -1e30f), t);
-    }
-  }
-  return RowSums{m, s, t};
-}
-// N more values; returns their maximum
-template <int N>
-__device__ inline float add_chunk(RowSums& r, const float* v, float c) {
-  float top = v[0];
-#pragma unroll
-  for (int i = 1; i < N; ++i) top = fmaxf(top, v[i]);
-  const float m = fmaxf(r.m, top), d = raise(r.m, m, c), f = __builtin_amdgcn_exp2f(-d);
-  r = sum_below<N>(m, r.s * f, (r.t - d * r.s) * f, v, c);
-  return top;
-}
-
 // Over a wavefront without a trip through LDS; every lane gets the result.  The lanes' order is fixed.
 template <int CTRL, int ROWS = 0xf>
 __device__ inline float dpp(float v, float other) {
@@ -162,11 +104,9 @@ __device__ inline RowSums merge_wave(const RowSums& r, float c) {
 // A row's results from its sums, written by one thread; x_target is read only with a target.  Returns ln S.
 __device__ inline float finish_row(const RowSums& r, const TokenOut& o, int row, bool has_target, float x_target, float inv_temp) {
   const bool empty = r.s == 0.f;  // nothing but -inf
-  const float c = inv_temp * kLog2e, mc = r.m * c, log_r = logf(r.s);
-  // relative to the maximum instead of the reference
-  const float log_s = empty ? -INFINITY : plain_exponent(mc) ? log_r + kLn2 * fmaf(-r.m, c, rintf(mc)) : log_r;
+  const float log_s = row_log_sum(r, inv_temp * kLog2e);
   o.logp[row] = !has_target ? 0.f : empty ? -INFINITY : (x_target - r.m) * inv_temp - log_s;
-  o.entropy[row] = empty ? 0.f : log_r - kLn2 * (r.t / r.s);
+  o.entropy[row] = row_entropy(r);
   o.row_stats[2 * row] = empty ? -INFINITY : r.m;
   o.row_stats[2 * row + 1] = log_s;
   return log_s;
