@@ -341,6 +341,8 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[i][j][e] += place == 4 * j + e ? add : 0.f;
         }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] *= q.inv_temp;
         if (__any(q.none || !whole)) {
 #pragma unroll
           for (int j = 0; j < NT; ++j)

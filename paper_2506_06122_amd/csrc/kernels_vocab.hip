@@ -379,9 +379,11 @@ __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] += at == e ? g.at_target : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] *= g.inv_temp;
     store(i, v);
   }
-  if (one >= 0) out[one] = narrow1(grad_of(to_f32(row.x[one]), c, g) + (one == g.target ? g.at_target : 0.f), V{});
+  if (one >= 0) out[one] = narrow1(grad_at(to_f32(row.x[one]), c, one, g), V{});
 }
 
 TokenParts layout(int rows, int vocab, int top, void* ws) {

@@ -89,3 +89,33 @@ ROW_SUMS_FN float row_log_sum(const RowSums& r, float c) {
   return r.s == 0.f ? -INFINITY : logf(r.s) - kLn2 * offset(r.m, c);
 }
 ROW_SUMS_FN float row_entropy(const RowSums& r) { return r.s == 0.f ? 0.f : logf(r.s) - kLn2 * (r.t / r.s); }
+
+// What a row's gradient needs beside its logits: T dx = p (a + b y2) (+ at_target at the target), y2 = log2 p.  1 / T comes last:
+// with small temperatures the factors would leave fp32's range where the result does not, and make a NaN of p = 0.
+struct RowGrad {
+  float m, l2, a, b, at_target, inv_temp;
+  int target;   // -1: none
+  bool none;    // the whole row is zero
+};
+ROW_SUMS_FN RowGrad row_grad_of(float m, float log_s, float entropy, float grad_logp, float grad_entropy, int target, float inv_temp) {
+  RowGrad r;
+  const float g = target < 0 ? 0.f : grad_logp, h = grad_entropy;
+  r.target = target;
+  r.m = m;
+  r.l2 = log_s * kLog2e;
+  r.none = (g == 0.f && h == 0.f) || log_s == -INFINITY;
+  r.a = -g - h * entropy;
+  r.b = -h * kLn2;
+  r.at_target = g;
+  r.inv_temp = inv_temp;
+  return r;
+}
+// T dx away from the target; c = log2(e) / T.  Where p = 0, a banned id's x = -inf among others, log2 p must not meet that 0 as an
+// infinity: 2^-256 is 0 in fp32 already.  A NaN stays one.
+ROW_SUMS_FN float grad_of(float x, float c, const RowGrad& r) {
+  const float y = fmaf(x - r.m, c, -r.l2);
+  return row_exp2(y) * fmaf(r.b, fmaxf(y, -256.f), r.a);
+}
+ROW_SUMS_FN float grad_at(float x, float c, int id, const RowGrad& r) {
+  return (grad_of(x, c, r) + (id == r.target ? r.at_target : 0.f)) * r.inv_temp;
+}

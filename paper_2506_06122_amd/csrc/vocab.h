@@ -51,32 +51,11 @@ struct TokenGrad {
 };
 void launch_token_logprobs_grad(const TokenGrad& a, hipStream_t s);
 
-// What a row's gradient needs beside its logits: dx = p (a + b y2) (+ at_target at the target), y2 = log2 p.
-struct RowGrad {
-  float m, l2, a, b, at_target;
-  int target;   // -1: none
-  bool none;    // the whole row is zero
-};
 __device__ inline RowGrad row_grad(const float* row_stats, const float* entropy, const float* grad_logp,
                                    const float* grad_entropy, const int* targets, float inv_temp, int vocab, int row) {
-  RowGrad r;
-  const float l = row_stats[2 * row + 1];
   const int t = targets ? targets[row] : -1;
-  r.target = t >= 0 && t < vocab ? t : -1;
-  const float gl = grad_logp[row], g = r.target < 0 ? 0.f : gl;
-  const float h = grad_entropy ? grad_entropy[row] : 0.f;
-  r.m = row_stats[2 * row];
-  r.l2 = l * kLog2e;
-  r.none = (g == 0.f && h == 0.f) || l == -INFINITY;
-  r.a = inv_temp * (grad_entropy ? -g - h * entropy[row] : -g);
-  r.b = -h * inv_temp * kLn2;
-  r.at_target = g * inv_temp;
-  return r;
-}
-// c = log2(e) / T.  A banned id has x = -inf: p = 0, and its log2 p must not meet that 0 as an infinity; a NaN stays one.
-__device__ inline float grad_of(float x, float c, const RowGrad& r) {
-  const float y = fmaf(x - r.m, c, -r.l2);
-  return __builtin_amdgcn_exp2f(y) * fmaf(r.b, fmaxf(y, -1e30f), r.a);
+  return row_grad_of(row_stats[2 * row], row_stats[2 * row + 1], grad_entropy ? entropy[row] : 0.f, grad_logp[row],
+                     grad_entropy ? grad_entropy[row] : 0.f, t >= 0 && t < vocab ? t : -1, inv_temp);
 }
 
 // Over a wavefront without a trip through LDS; every lane gets the result.  The lanes' order is fixed.

@@ -107,3 +107,18 @@ def test_lm_head_of_whole_numbers(rows, vocab, temperature):
     for a, b in ((dh, want_h), (dw, want_w)):
         # two roundings to bf16, each at most 2^-8 relative to its value: their norms add up to less than 2^-7
         assert np.linalg.norm(a.double().cpu().numpy() - b) <= 2 * BF * np.linalg.norm(b)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("temperature", [1e-9, 1e-10, 1e-20, 1e-37])
+def test_gradients_at_the_smallest_temperatures(temperature, dtype):
+    """The entropy's part of a masked value's gradient is 0, however large 1 / T."""
+    x = masked(5003, [-65504.0, -1e30, -np.inf], 11)
+    x[::2, 100:200] = x.max(1)[::2, None]  # ties: a distribution over some
+    check(x, dtype, temperature, 3, 5)
+
+
+@pytest.mark.parametrize("temperature", [1e-10, 1e-30])
+def test_lm_head_gradients_at_the_smallest_temperatures(temperature):
+    for rows, vocab in ((5, 1000), (130, 3001)):
+        test_lm_head_of_whole_numbers(rows, vocab, temperature)

@@ -5,3 +5,7 @@ from test_host_tile_grid import run_driver
 
 def test_sums_over_the_range_of_logits_and_temperatures(tmp_path):
     assert int(run_driver("row_sums_driver", tmp_path).split()[0]) > 100_000
+
+
+def test_gradients_over_the_range_of_logits_and_temperatures(tmp_path):
+    assert int(run_driver("row_grad_driver", tmp_path).split()[0]) > 100_000
