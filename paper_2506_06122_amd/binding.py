@@ -641,8 +641,6 @@ def rollout_token_logprobs_grad(logits, targets, row_stats, entropy, grad_logp, 
     gl = _vector(grad_logp, "grad_logp", device, torch.float32, rows)
     ge = _vector(grad_entropy, "grad_entropy", device, torch.float32, rows)
     out_stride = _rows(out, "out", device, logits.dtype, logits.shape) if out is not None else vocab
-    if out is not None and out.data_ptr() == logits.data_ptr():
-        out_stride = stride  # one row: any stride is its own
     with _On(device, stream) as s:
         if out is None:
             out = torch.empty(rows, vocab, dtype=logits.dtype, device=device)
