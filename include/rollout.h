@@ -377,7 +377,7 @@ int rollout_policy_loss(int32_t n_seqs, const int32_t *cu_seqlens, const float *
  *   top_ids, top_logp [rows][top]: the `top` greatest values, greatest first, equal ones by ascending id, NaN last, and
  *     their log-probs; 0 <= top <= min(vocab, ROLLOUT_TOP_MAX), both NULL with 0
  * A row of -inf alone: logp -inf, entropy 0, row_stats (-inf, -inf), alternatives of log-prob -inf.  A row with a NaN or
- * +inf has NaN for all of its numbers. */
+ * +inf has NaN for all of its numbers: logp (with a target), entropy, row_stats, top_logp; top_ids are in the order above. */
 #define ROLLOUT_TOP_MAX 64
 int64_t rollout_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t top);
 int rollout_token_logprobs(const void *logits, int32_t dtype, int32_t rows, int32_t vocab, int64_t row_stride,

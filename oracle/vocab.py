@@ -32,8 +32,7 @@ def token_logprobs(x, targets, temperature, top=0):
         if np.isnan(x[r]).any() or np.isposinf(x[r]).any():
             logp[r] = np.nan if has else 0.0
             entropy[r] = np.nan
-            finite = x[r][~np.isnan(x[r])]
-            stats[r] = np.max(finite) if len(finite) else np.nan, np.nan
+            stats[r] = np.nan
             alt[r] = np.nan
         else:
             s = _softmax(x[r], temperature)
