@@ -313,7 +313,6 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
     // bf16, through LDS so that rows leave as whole lines
     char* mine = lds + wave * OUT_WAVE;
     const RowGrad* row_grads = (const RowGrad*)(lds + OUT);
-    const float c = p.inv_temp * kLog2e;
     if constexpr (TO == TO_GRAD) {
       for (int ml = threadIdx.x; ml < BM; ml += NW * 64) {
         RowGrad q{};
@@ -333,7 +332,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] = grad_of(acc[i][j][e], c, q);
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = grad_of(acc[i][j][e], q);
         if (__any(here)) {
           const float add = here ? q.at_target : 0.f;
 #pragma unroll

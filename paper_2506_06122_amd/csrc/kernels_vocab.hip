@@ -194,7 +194,7 @@ struct TokenParts {
 __device__ inline void store_top(const TokenOut& o, int row, int rank, unsigned long long key, float m, float log_s, float inv_temp) {
   const long long at = (long long)row * o.top + rank;
   o.top_ids[at] = (int)~(unsigned)key;
-  o.top_logp[at] = log_s == -INFINITY ? -INFINITY : (key_value((unsigned)(key >> 32)) - m) * inv_temp - log_s;
+  o.top_logp[at] = row_logp(key_value((unsigned)(key >> 32)), m, inv_temp, log_s);
 }
 
 // STREAM: past the caches
@@ -350,7 +350,6 @@ __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
   const RowSlice<V> row((const V*)a.in.logits + r * a.in.stride, a.in.vocab, part, parts);
   V* out = (V*)a.out + r * a.out_stride;
   const RowGrad g = row_grad(a.row_stats, a.entropy, a.grad_logp, a.grad_entropy, a.in.targets, a.in.inv_temp, a.in.vocab, r);
-  const float c = a.in.inv_temp * kLog2e;
   auto store = [&](int i, const float* v) {
     if constexpr (SAME) {
       u32x4* to = (u32x4*)(out + row.id(i));
@@ -373,7 +372,7 @@ __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
     float v[E];
     widen(STREAM ? __builtin_nontemporal_load((const u32x4*)(row.x + row.id(i))) : row.vec(i), v, V{});
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = grad_of(v[e], c, g);
+    for (int e = 0; e < E; ++e) v[e] = grad_of(v[e], g);
     const unsigned at = (unsigned)(g.target - row.id(i));
     if (at < E) {
 #pragma unroll
@@ -383,7 +382,7 @@ __global__ __launch_bounds__(T) void token_grad_kernel(TokenGrad a, int parts) {
     for (int e = 0; e < E; ++e) v[e] *= g.inv_temp;
     store(i, v);
   }
-  if (one >= 0) out[one] = narrow1(grad_at(to_f32(row.x[one]), c, one, g), V{});
+  if (one >= 0) out[one] = narrow1(grad_at(to_f32(row.x[one]), one, g), V{});
 }
 
 TokenParts layout(int rows, int vocab, int top, void* ws) {

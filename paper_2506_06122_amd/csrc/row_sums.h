@@ -90,18 +90,31 @@ ROW_SUMS_FN float row_log_sum(const RowSums& r, float c) {
 }
 ROW_SUMS_FN float row_entropy(const RowSums& r) { return r.s == 0.f ? 0.f : logf(r.s) - kLn2 * (r.t / r.s); }
 
+// (x - m) scale as fma(x, part, -m part) (scale / part): where the scale is below 1 a difference past fp32's range may yet give a
+// value inside it, and halves leave every other difference as it is.
+ROW_SUMS_FN float part_of(float scale) { return scale < 1.f ? 0.5f : 1.f; }
+// ln p of a value whose x is given
+ROW_SUMS_FN float row_logp(float x, float m, float inv_temp, float log_s) {
+  if (log_s == -INFINITY) return -INFINITY;  // a row of nothing but -inf
+  const float k = part_of(inv_temp);
+  return fmaf(fmaf(x, k, -m * k), inv_temp / k, -log_s);
+}
+
 // What a row's gradient needs beside its logits: T dx = p (a + b y2) (+ at_target at the target), y2 = log2 p.  1 / T comes last:
 // with small temperatures the factors would leave fp32's range where the result does not, and make a NaN of p = 0.
 struct RowGrad {
-  float m, l2, a, b, at_target, inv_temp;
-  int target;   // -1: none
-  bool none;    // the whole row is zero
+  float k, mk, ck;  // part, maximum times part, log2(e) / T / part
+  float l2, a, b, at_target, inv_temp;
+  int target;       // -1: none
+  bool none;        // the whole row is zero
 };
 ROW_SUMS_FN RowGrad row_grad_of(float m, float log_s, float entropy, float grad_logp, float grad_entropy, int target, float inv_temp) {
   RowGrad r;
-  const float g = target < 0 ? 0.f : grad_logp, h = grad_entropy;
+  const float g = target < 0 ? 0.f : grad_logp, h = grad_entropy, c = inv_temp * kLog2e;
   r.target = target;
-  r.m = m;
+  r.k = part_of(c);
+  r.mk = m * r.k;
+  r.ck = c / r.k;
   r.l2 = log_s * kLog2e;
   r.none = (g == 0.f && h == 0.f) || log_s == -INFINITY;
   r.a = -g - h * entropy;
@@ -110,12 +123,12 @@ ROW_SUMS_FN RowGrad row_grad_of(float m, float log_s, float entropy, float grad_
   r.inv_temp = inv_temp;
   return r;
 }
-// T dx away from the target; c = log2(e) / T.  Where p = 0, a banned id's x = -inf among others, log2 p must not meet that 0 as an
-// infinity: 2^-256 is 0 in fp32 already.  A NaN stays one.
-ROW_SUMS_FN float grad_of(float x, float c, const RowGrad& r) {
-  const float y = fmaf(x - r.m, c, -r.l2);
+// T dx away from the target.  Where p = 0, a banned id's x = -inf among others, log2 p must not meet that 0 as an infinity: 2^-256
+// is 0 in fp32 already.  A NaN stays one.
+ROW_SUMS_FN float grad_of(float x, const RowGrad& r) {
+  const float y = fmaf(fmaf(x, r.k, -r.mk), r.ck, -r.l2);
   return row_exp2(y) * fmaf(r.b, fmaxf(y, -256.f), r.a);
 }
-ROW_SUMS_FN float grad_at(float x, float c, int id, const RowGrad& r) {
-  return (grad_of(x, c, r) + (id == r.target ? r.at_target : 0.f)) * r.inv_temp;
+ROW_SUMS_FN float grad_at(float x, int id, const RowGrad& r) {
+  return (grad_of(x, r) + (id == r.target ? r.at_target : 0.f)) * r.inv_temp;
 }

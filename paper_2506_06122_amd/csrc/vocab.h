@@ -84,7 +84,7 @@ __device__ inline RowSums merge_wave(const RowSums& r, float c) {
 __device__ inline float finish_row(const RowSums& r, const TokenOut& o, int row, bool has_target, float x_target, float inv_temp) {
   const bool empty = r.s == 0.f;  // nothing but -inf
   const float log_s = row_log_sum(r, inv_temp * kLog2e);
-  o.logp[row] = !has_target ? 0.f : empty ? -INFINITY : (x_target - r.m) * inv_temp - log_s;
+  o.logp[row] = has_target ? row_logp(x_target, r.m, inv_temp, log_s) : 0.f;
   o.entropy[row] = row_entropy(r);
   o.row_stats[2 * row] = empty ? -INFINITY : r.s != r.s ? r.s : r.m;  // (the maximum passes NaN by)
   o.row_stats[2 * row + 1] = log_s;

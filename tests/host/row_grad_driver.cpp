@@ -32,7 +32,7 @@ static void check(const char* kind, const std::vector<float>& x, float T, float 
     const long double mag = (p > 0 ? fabsl(lp) + 2 * log_s : 0) + 4, size = fabsl(gt) + fabsl(h) * (mag + H);
     const long double tol = (size * (p * (4 * u * mag + 8 * u) + ldexpl(1, -126)) + 8 * u * fabsl(gt)) / T + u * fabsl(want) + ldexpl(1, -126);
     if (fabsl(want) + tol > 3.4e38L) continue;  // not a value of the type
-    const float got = r.none ? 0.f : grad_at(x[i], c, i, r);
+    const float got = r.none ? 0.f : grad_at(x[i], i, r);
     if (!(fabsl(got - want) <= tol)) {
       std::fprintf(stderr, "%s, %d values, T %g, g %g, h %g, target %d: value %d, logit %g, is %g of %Lg +- %Lg\n", kind, V, T, g, h, target, i, x[i], got,
                    want, tol);
@@ -60,6 +60,12 @@ int main() {
             std::vector<float> x(V);
             for (int i = 0; i < V; ++i) x[i] = i % 3 == 1 ? fill : 5.f * uniform(seed) - 2.5f;
             for (int target : {-1, 0, V - 1}) check("masked", x, T, g, h, target);
+          }
+          for (int i = 0; i < V; ++i) {  // differences past fp32's range
+            std::vector<float> x(V, 2.5f);
+            x[i] = kLowest;
+            x[V - 1 - i] = 3.3e38f;
+            check("wide", x, T, g, h, i);
           }
           for (float size : {1.f, 1e3f, 1e30f}) {
             std::vector<float> x(V);

@@ -66,6 +66,14 @@ static void check(const Row& row, float T) {
         const float got_s = row_log_sum(r, c), got_h = row_entropy(r);
         const double off_s = empty ? (got_s == -INFINITY ? 0 : 1) : std::fabs(got_s - log_s), off_h = std::fabs(got_h - entropy);
         const double tol_s = (n + 8) * u + u * std::fabs(empty ? 0 : log_s), tol_h = tol_s + (2 * n + 32) * u * std::log(V + 1.0);
+        for (int i = 0; i < V && !empty; i += 1 + V / 16) {  // ln p: the difference's, the product's and 1 / T's roundings beside ln S
+          const double lp = (double)(((long double)row.x[i] - m) / T) - log_s, got = row_logp(row.x[i], r.m, inv, got_s);
+          const bool past = lp < -0x1.fffffep127;  // below fp32's range
+          if (past ? got > -0x1.ffffe0p127 : !(std::fabs(got - lp) <= tol_s + 4 * u * (std::fabs(lp) + 2 * std::fabs(log_s)) || got == lp)) {
+            std::fprintf(stderr, "%s %g, %d values, T %g: ln p of %g is %g of %g\n", row.kind, row.at, V, T, row.x[i], got, lp);
+            std::exit(1);
+          }
+        }
         if (!(off_s <= tol_s) || !(off_h <= tol_h) || (!empty && r.m != m)) {
           std::fprintf(stderr, "%s %g, %d values, T %g, %d threads, walk %d, join %d: max %g of %g, ln S %g of %g, entropy %g of %g\n", row.kind,
                        row.at, V, T, threads, walk, join, r.m, m, got_s, log_s, got_h, entropy);
@@ -98,6 +106,13 @@ int main() {
           }
           check({"partly", fill, x}, T);
         }
+      }
+      // differences past fp32's range
+      for (int i = 0; i < V; i += 1 + V / 8) {
+        std::vector<float> x(V, 2.5f);
+        x[i] = kLowest;
+        x[V - 1 - i] = 3.3e38f;
+        check({"wide", (float)i, x}, T);
       }
       // ordinary logits, and larger ones
       for (float size : {1.f, 25.f, 1e3f, 6e4f, 1e9f, 1e30f}) {

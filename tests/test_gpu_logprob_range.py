@@ -122,3 +122,12 @@ def test_gradients_at_the_smallest_temperatures(temperature, dtype):
 def test_lm_head_gradients_at_the_smallest_temperatures(temperature):
     for rows, vocab in ((5, 1000), (130, 3001)):
         test_lm_head_of_whole_numbers(rows, vocab, temperature)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("temperature", [1e9, 1e30, 3e38])
+def test_large_temperatures(temperature, dtype):
+    """Banned ids stay banned where log2(e) / T is below fp32's normal range."""
+    x = masked(5003, [-65504.0, -1e30, -3e38, -np.inf], 12)
+    x[:, 7] = 3e38 if dtype == "float32" else 2.5
+    check(x, dtype, temperature, 3, 6)
