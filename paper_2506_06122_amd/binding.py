@@ -606,7 +606,9 @@ def rollout_token_logprobs(logits, targets=None, *, temperature=1.0, top=0, stre
     """Log-probs of `targets` (int32 [rows], or None) under logits [rows][vocab] (CUDA, float32 / bfloat16 / float16; rows
     may be strided), with entropies and the `top` most likely alternatives.  Returns new CUDA tensors (logp, entropy,
     row_stats [rows][2], top_ids int32 [rows][top], top_logp [rows][top]), the last two None without `top`.  Enqueues on
-    `stream` (a handle; default: PyTorch's current stream) and does not wait: keep the inputs until that work is done."""
+    `stream` (a handle; default: PyTorch's current stream) and does not wait: keep the inputs until that work is done.
+    Autograd does not see this call nor the others here: results carry no graph, whatever the inputs require, and the
+    *_grad calls are the way back."""
     import torch
     lib, device = load_library(), logits.device
     stride = _rows(logits, "logits", device)

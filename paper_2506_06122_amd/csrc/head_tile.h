@@ -113,8 +113,8 @@ constexpr HeadTile head_tile(int M, int N) {
 }
 // the gradients' first product writes whole slices of rows, zeros included (16 x 256 tiles, 7 rows: 208 us, four times the
 // workgroups, where 64 x 256 take 119), and the device alone knows how many rows there are (160 rows, a quarter without
-// gradient, 151936 x 1536, all three products: 445 us with 128 x 128 tiles here, 474 with 256 x 256; 128 x 256 1 to 2 %
-// less than 128 x 128: 187 rows 477 -> 468, 128 rows x 152064 x 3584 968 -> 956)
+// gradient, 151936 x 1536, all three products: 445 us with 128 x 128 tiles here, 474 with 256 x 256; 128 x 256 a
+// little less than 128 x 128, seven runs in turn each: 187 rows 468-488 and 473-487, 128 rows x 152064 x 3584 951-957 and 960-974)
 constexpr HeadTile head_tile_logits(int M, int N) {
   if (M <= 64) return {64, 256};
   if (M <= 256 && head_ceil(N, 256) >= 192) return {128, 256};
@@ -123,7 +123,7 @@ constexpr HeadTile head_tile_logits(int M, int N) {
 }
 // the gradients' second and third product: K is long in grad_hidden's, which is cut along it instead, and short in
 // grad_head's with few rows, where two small workgroups to a CU hide each other's start and end (32 rows x 152064 x 3584 723
-// -> 655 us in all, 151936 x 1536 with 187 rows 497 -> 469, with 400 684 -> 668, but with 613 770 either way)
+// -> 655 us in all, 151936 x 1536 with 187 rows 497 -> 469, with 400 691 -> 675, but with 613 775 to 782 either way)
 // (one row of tiles of grad_hidden: 128 x 256 and three stages, 64 rows x 152064 x 3584 715 -> 690 us in all)
 constexpr HeadTile head_tile_hidden(int M) { return M <= 128 ? HeadTile{128, 256} : M <= 256 ? HeadTile{128, 128} : HeadTile{256, 256}; }
 constexpr HeadTile head_tile_head(int K) { return K <= 512 ? HeadTile{128, 128} : HeadTile{256, 256}; }

@@ -284,7 +284,9 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedGrad a, EmbedSort q
   }
 }
 
-// A run that leaves its chunk: the chunk in which it begins takes the shares of the following ones, in order.
+// A run that leaves its chunk: the chunk in which it begins takes the shares of the following ones, in order, a wavefront to 512
+// columns: a long run is a chain of loads (x 3584 bf16, all three launches in place, us: 16384 rows of one id 150, of mixed ids
+// 118; 10^5 rows of mixed ids 454, a fifth of them one id 630, all of them 1228).
 template <typename G, bool VEC>
 __global__ __launch_bounds__(64) void embed_join_kernel(EmbedGrad a, EmbedSort q, int kChunk) {
   constexpr int E = VEC ? 8 : 1;

@@ -8,9 +8,10 @@
 // each operand lies with its rows or with the summed index outermost, as the caller or the previous launch left it -
 // fragments of the second kind are transposed on their way out of LDS - so that nothing is transposed in memory.
 //
-// 4096 x 152064 x 3584: 3.21 to 3.37 ms, 1.32 to 1.39 PFLOP/s by the card (matrix instructions two thirds of the time, the
+// 4096 x 152064 x 3584: 3.25 to 3.37 ms, 1.32 to 1.37 PFLOP/s by the card (matrix instructions two thirds of the time, the
 // clock at 1.9 to 2.0 GHz under them); its gradients with respect to three quarters of the rows, three products, 8.0 to 8.4 ms, 1.20 to 1.25 PFLOP/s: slices with K
-// outermost take a tenth longer.  7 x 151936 x 1536: 89 us, 5.3 TB/s of W.
+// outermost take a tenth longer.  7 x 151936 x 1536: 90 us, 5.2 TB/s of W.  In between a tile's start and end show, with 5 to 24
+// stages to it and one workgroup to a CU: 160 x 151936 x 1536 136 us, 300 192, 613 305; W's bytes take 74, the products 51 to 197.
 #include "vocab.h"
 
 #include <algorithm>
@@ -223,8 +224,9 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT >= 32 || S > 2 ? 1 : 2) void h
     auto half_stage = [&](auto halfc, auto copiesc, const char* st) __attribute__((always_inline)) {
       constexpr int H = decltype(halfc)::value, NS = NR + (decltype(copiesc)::value ? L : 0);
       unrolled([&](auto qc) __attribute__((always_inline)) {
-        // reads alone are through in half the time, so that the barrier does not wait for the last of them; copies evenly, as fast
-        // as the CU takes them (4096 x 152064 x 3584: 3.27 -> 3.23 ms; both within half the time 3.42)
+        // reads alone are through in half the time, so that the barrier need not wait for the last of them (no difference that two runs
+        // in turn would show: 4096 x 152064 x 3584 3.32 ms, reads spread over all of it 3.33); copies evenly, as fast as the CU
+        // takes them (both within half the time 3.42)
         constexpr int q = decltype(qc)::value, OVER = decltype(copiesc)::value ? NM : NM / 2;
         constexpr int u0 = q >= OVER ? NS : (q * NS + OVER - 1) / OVER, u1 = q + 1 >= OVER ? NS : ((q + 1) * NS + OVER - 1) / OVER;
         mul(H, q);

@@ -2,9 +2,10 @@
 //
 //   y_v = x_v log2(e) / T - r,  S = sum 2^y,  ln p_v = ln2 y_v - ln S,  H = ln S - ln2 (sum y 2^y) / S, for any r
 //
-// One pass over the row: every thread keeps the maximum it has seen, and its two sums relative to that (RowSums); a chunk of
+// One pass over the row: every thread keeps the maximum it has seen, and its two sums relative to that (row_sums.h); a chunk of
 // values is taken relative to the new maximum, the old sums are scaled once a chunk.  The pass is bound by memory; the
-// arithmetic (9 issue slots per value, the exponential counting four) comes next.
+// arithmetic (9 issue slots per value, the exponential counting four) comes next.  Chunks that hold a value of -inf are summed
+// twice (a fiftieth of the values, so nearly every chunk: 2048 x 152064 bf16 146 us instead of 96).
 //
 // Alternatives ride along: every thread notes the maximum of each of kSegments runs of its values.  The K-th largest of
 // these is a bound that K values reach, and every value that reaches it lies in a run whose maximum does.  So only those
@@ -13,7 +14,8 @@
 //
 // A row belongs to one workgroup where rows are enough; fewer are cut into parts whose results a second launch joins.
 //
-// 2048 x 152064 bf16: 94 us without alternatives, 6.6 TB/s; 107 us with 8.  A lone row of 151936 fp32 with 20: 7.4 and 6.7 us.
+// 2048 x 152064 bf16, calls in a loop: 95 us without alternatives, 6.5 TB/s (some processes 117); 109 to 111 with 8, a first call
+// after other work 118.  A lone row of 151936 fp32 with 20: 7.5 to 8.6 and 7.0 us.
 #include "vocab.h"
 #include "vocab_vec.h"
 
