@@ -62,12 +62,10 @@ def test_rows_of_the_lowest_value(temperature):
         check(x, dtype, temperature, 3, 2)
 
 
-@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
-@pytest.mark.parametrize("temperature", [1e-3, 1e-5, 1e-6, 1e-7, 1e-8])
+# (float16 does not hold gradients of more than 65504)
+@pytest.mark.parametrize("temperature,dtype", [(1e-3, "float16")] + [(t, d) for t in (1e-3, 1e-5, 1e-6, 1e-7, 1e-8) for d in ("float32", "bfloat16")])
 @pytest.mark.parametrize("size", [2.5, 1e3, 1.5e4])
 def test_small_temperatures(size, temperature, dtype):
-    if dtype == "float16" and temperature < 1e-3:
-        pytest.skip("gradients of 1 / T do not fit the type")
     rng = np.random.default_rng(int(size))
     x = rng.normal(0, 1, (40, 9001)).astype(np.float32)
     x = np.clip(x, -4, 4) * np.float32(size)
